@@ -332,6 +332,85 @@ cats_status cats_calibrate_stack(const cats_layer* layers, int32_t L, const floa
 cats_status cats_rmsnorm(const float* x, float* xn, int32_t B, int32_t d, float eps,
                          void* stream);
 
+/* ---- 8-bit operands --------------------------------------------------------
+ * Linear layers on e4m3 values (OCP FP8 E4M3: 1 sign, 4 exponent, 3 mantissa
+ * bits, largest 448, no infinity) with a scale for each block of CATS_FP8_BLOCK
+ * columns, for one row or a whole prompt of them: half the bytes of bf16
+ * weights and twice its matrix rate.  A matrix of rows x cols is held as
+ *   q       dev [rows x ld] e4m3, ld = cats_fp8_ld(cols) = cols rounded up to
+ *           a multiple of CATS_FP8_BLOCK; zero from column cols on.  A matrix
+ *           whose width is such a multiple is a plain [rows x cols] array.
+ *   scale   dev [ceil(rows / block_rows) x ld / CATS_FP8_BLOCK]; the element
+ *           (r, c) has the value q[r, c] * scale[r / block_rows, c / CATS_FP8_BLOCK].
+ *           block_rows is 1 for the rows of x, CATS_FP8_BLOCK for weights.
+ * Scales are fp32 (CATS_SCALE_F32) or powers of two (CATS_SCALE_E8M0, OCP E8M0:
+ * a byte e stands for 2^(e - 127), 255 for NaN), which the matrix
+ * instructions apply by themselves.
+ * The calls that write such matrices take, with a the block's largest finite
+ * magnitude, the scale a / 448 in fp32 (2^-126 if that is less), or the
+ * smallest 2^e with a <= 448 * 2^e and e >= -126, and 1 where a is 0; q is the
+ * nearest e4m3 value of element / scale (ties to even; the fp32 quotient may be
+ * off by 1.5 of its last bits).  An infinite or NaN element becomes e4m3's NaN;
+ * the block's other elements are what they are without it.
+ * All four calls are enqueue only and may be captured in a graph. */
+#define CATS_FP8_BLOCK 128
+typedef enum { CATS_SCALE_F32 = 0, CATS_SCALE_E8M0 = 1 } cats_scale_type;
+/* Most rows (of x, or outputs of a weight) and columns of such a matrix. */
+#define CATS_MAX_FP8_ROWS (1 << 20)
+#define CATS_MAX_FP8_COLS 65536
+
+/* Row pitch of a matrix of `cols` columns; 0 outside [1, CATS_MAX_FP8_COLS].
+ * Pure host arithmetic. */
+int32_t cats_fp8_ld(int32_t cols);
+
+/* Quantise x (dev [rows x cols] of dtype CATS_F32 or CATS_BF16, aligned to
+ * its elements) with a scale for each block_rows x CATS_FP8_BLOCK elements,
+ * block_rows 1 (rows of x) or CATS_FP8_BLOCK (weights [n x k], row j = output
+ * j: W_gate^T and W_up^T as they are, W_down through cats_pack_weights).  q is
+ * 16-byte aligned; x, q and scale must not overlap. */
+cats_status cats_quantize_fp8(const void* x, int32_t dtype, int32_t rows, int32_t cols, int32_t block_rows,
+                              int32_t stype, void* q, void* scale, void* stream);
+
+/* The residual's addition, RMSNorm and the 8-bit output in one pass:
+ *   s = x + residual,  q, scale = quantise(gain * s / sqrt(mean(s^2) + eps))
+ * with one scale per row and CATS_FP8_BLOCK columns.
+ *   x         dev [N x d], fp32 or bf16 (dtype): a layer's output
+ *   residual  dev [N x d] fp32, the residual stream; NULL: s = x
+ *   gain      dev [d] fp32; NULL: 1 (as cats_rmsnorm)
+ *   sum_out   dev [N x d] fp32, receives s; NULL: not written.  May be the
+ *             residual itself, or x if that is fp32.
+ * The sum, the mean and the normalised row are fp32 and never rounded to less
+ * before q.  Rows whose sum of squares overflows fp32 become 0, as cats_rmsnorm's.
+ * 1 <= N <= CATS_MAX_FP8_ROWS, 1 <= d <= CATS_MAX_FP8_COLS, eps >= 0. */
+cats_status cats_rmsnorm_fp8(const void* x, int32_t dtype, const float* residual, const float* gain, int32_t N,
+                             int32_t d, float eps, int32_t stype, float* sum_out, void* q, void* scale, void* stream);
+
+/* The gate of a CATS block with an 8-bit output: for gate_up dev [N x 2m] (a
+ * row's m gate values g = x W_gate, then its m up values u = x W_up; fp32 or bf16)
+ *   v = SiLU(g),  h = v * u where |v| >= t, else 0,  q, scale = quantise(h)
+ * with one scale per row and CATS_FP8_BLOCK neurons.  t >= 0 as in
+ * cats_mlp_forward (NaN v is kept; t = 0 keeps every neuron, t = +inf none). */
+cats_status cats_silu_mul_fp8(const void* gate_up, int32_t dtype, int32_t N, int32_t m, float t, int32_t stype, void* q,
+                              void* scale, void* stream);
+
+/* Linear layer on 8-bit operands, sums in fp32:
+ *   y[r, j] = residual[r, j] + sum_b xs[r, b] wscale[j / 128, b] sum_{c in block b} xq[r, c] wq[j, c]
+ *   xq, xs      rows of x: [N x ld], block_rows 1
+ *   wq, wscale  the weight, row j = output j: [n x ld], block_rows CATS_FP8_BLOCK
+ *   k           columns of both before padding; stype is both scales' type
+ *   residual    dev [N x n] of ydtype or NULL;  y dev [N x n], CATS_F32 or
+ *               CATS_BF16 (rounded once, after the residual).  y may be the
+ *               residual, and overlaps nothing else.
+ * xq, wq, y and residual 16-byte aligned.  NaN in q or a scale makes NaN of the
+ * outputs it reaches; scales may be any number of their type whose product of
+ * two, which is formed first, is in fp32's range.  1 <= N, n <=
+ * CATS_MAX_FP8_ROWS, 1 <= k <= CATS_MAX_FP8_COLS.  Workspace:
+ * cats_linear_fp8_workspace_bytes(N, n, k). */
+size_t cats_linear_fp8_workspace_bytes(int32_t N, int32_t n, int32_t k);
+cats_status cats_linear_fp8(const void* xq, const void* xs, int32_t N, const void* wq, const void* wscale, int32_t n,
+                            int32_t k, int32_t stype, const void* residual, void* y, int32_t ydtype, void* ws,
+                            size_t ws_bytes, void* stream);
+
 /* Attainable read bandwidth (a measurement aid; nothing of the method):
  * streams `bytes` of device memory at `buf` (16-byte aligned, a positive
  * multiple of 16, at most 1 GiB) with the 16-byte non-temporal loads the

@@ -9,6 +9,9 @@ binding.  Build with ``python -m paper_2404_08763_amd.build``.
 """
 from ._lib import (  # noqa: F401
     CATS_BF16,
+    CATS_SCALE_E8M0,
+    CATS_SCALE_F32,
+    FP8_BLOCK,
     CATS_UNFUSED_INDEX,
     CATS_UNFUSED_MASK,
     CATS_F32,
@@ -16,17 +19,23 @@ from ._lib import (  # noqa: F401
     Layer,
     calib_activations,
     calibrate_threshold,
+    fp8_ld,
     layer_from_math,
     lib_path,
+    linear_fp8,
+    linear_fp8_workspace,
     mlp_dense,
     mlp_forward,
     mlp_forward_topk,
     mlp_forward_unfused,
     pack_weights,
+    quantize_fp8,
     raw,
     Stack,
     calibrate_stack,
     rmsnorm,
+    rmsnorm_fp8,
+    silu_mul_fp8,
     sparse_input_gemv,
     sparse_input_workspace,
     stack_forward,

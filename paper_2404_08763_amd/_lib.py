@@ -21,6 +21,9 @@ _LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libcats.so
 
 CATS_F32 = 0
 CATS_BF16 = 1
+CATS_SCALE_F32 = 0
+CATS_SCALE_E8M0 = 1
+FP8_BLOCK = 128  # columns (and, for weights, rows) that share a scale
 # size of the fixed scratch array behind cats_mlp_forward_noalloc
 NOALLOC_SCRATCH_BYTES = 32 << 20
 STATUS_NAMES = {
@@ -83,6 +86,12 @@ _SIGNATURES = {
     "cats_unfused_workspace_bytes": ([_i32, _i32, _i32], _sz),
     "cats_mlp_forward_unfused": ([ctypes.POINTER(_Layer), _vp, _i32, _f32, _i32, _vp, _vp, _vp, _sz, _vp], _i32),
     "cats_rmsnorm": ([_vp, _vp, _i32, _i32, _f32, _vp], _i32),
+    "cats_fp8_ld": ([_i32], _i32),
+    "cats_quantize_fp8": ([_vp, _i32, _i32, _i32, _i32, _i32, _vp, _vp, _vp], _i32),
+    "cats_rmsnorm_fp8": ([_vp, _i32, _vp, _vp, _i32, _i32, _f32, _i32, _vp, _vp, _vp, _vp], _i32),
+    "cats_silu_mul_fp8": ([_vp, _i32, _i32, _i32, _f32, _i32, _vp, _vp, _vp], _i32),
+    "cats_linear_fp8_workspace_bytes": ([_i32, _i32, _i32], _sz),
+    "cats_linear_fp8": ([_vp, _vp, _i32, _vp, _vp, _i32, _i32, _i32, _vp, _vp, _i32, _vp, _sz, _vp], _i32),
     "cats_stream_read": ([_vp, _sz, _i32, _i32, _i32, _vp, _vp], _i32),
     "cats_timer_enable": ([_i32], _i32),
     "cats_timer_reset": ([], _i32),
@@ -132,6 +141,7 @@ def _stream_of_torch() -> Callable[[], int]:
 
 
 _stream = _stream_of_torch()
+_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
 def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
@@ -521,6 +531,170 @@ def rmsnorm(x: torch.Tensor, eps: float = 1e-5, out: Optional[torch.Tensor] = No
     B = _rows(x)
     d = int(x.shape[-1])
     _check(raw().cats_rmsnorm(_ptr(x), _ptr(out), B, d, float(eps), _stream()))
+    return out
+
+
+# ---- 8-bit operands ---------------------------------------------------------
+# e4m3 values [rows, ld] (ld: the columns rounded up to FP8_BLOCK, zeros behind
+# them) with a scale for each 1 (rows of x) or FP8_BLOCK (weights) rows by
+# FP8_BLOCK columns, torch.float32 or torch.float8_e8m0fnu (powers of two).
+
+_SCALE_TYPES = {torch.float32: CATS_SCALE_F32, torch.float8_e8m0fnu: CATS_SCALE_E8M0}
+
+
+def fp8_ld(cols: int) -> int:
+    """Columns of the e4m3 array of a matrix of `cols` columns."""
+    return (cols + FP8_BLOCK - 1) // FP8_BLOCK * FP8_BLOCK
+
+
+def _blocks(rows: int) -> int:
+    return (rows + FP8_BLOCK - 1) // FP8_BLOCK
+
+
+def _stype(dt: torch.dtype) -> int:
+    st = _SCALE_TYPES.get(dt)
+    if st is None:
+        raise ValueError(f"scales are torch.float32 or torch.float8_e8m0fnu, not {dt}")
+    return st
+
+
+def _shape_is(t: torch.Tensor, shape: tuple, name: str) -> None:
+    if t.shape != shape:
+        raise ValueError(f"{name} must be {list(shape)}, has shape {list(t.shape)}")
+
+
+def _here(name: str, t: torch.Tensor, dtype: torch.dtype, device: int) -> None:
+    """A contiguous tensor of that type on the current device, on whose stream
+    the call runs."""
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a device tensor")
+    if t.dtype != dtype:
+        raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    if t.get_device() != device:
+        raise ValueError(f"{name} is on device {t.get_device()}, the current device is {device}")
+
+
+def _fp8_io(x: torch.Tensor, rows: int, cols: int, block_rows: int, scale_dtype: torch.dtype, out):
+    """Checks a quantising call's input and returns its q and scale (out's, or
+    new ones) and the device they are on."""
+    if x.dtype is not torch.float32 and x.dtype is not torch.bfloat16:
+        raise ValueError(f"the input must be torch.float32 or torch.bfloat16, got {x.dtype}")
+    qs = (rows, fp8_ld(cols))
+    ss = (rows if block_rows == 1 else _blocks(rows), qs[1] // FP8_BLOCK)
+    if out is not None:
+        q, scale = out
+        _shape_is(q, qs, "q")
+        _shape_is(scale, ss, "scale")
+        scale_dtype = scale.dtype
+    _stype(scale_dtype)
+    if not x.is_cuda:
+        raise ValueError("the input must be a device tensor")
+    if out is None:
+        q = torch.empty(qs, dtype=torch.float8_e4m3fn, device=x.device)
+        scale = torch.empty(ss, dtype=scale_dtype, device=x.device)
+    device = _device()
+    _here("the input", x, x.dtype, device)
+    _here("q", q, torch.float8_e4m3fn, device)
+    _here("scale", scale, scale.dtype, device)
+    return q, scale, device
+
+
+def _two_dims(x: torch.Tensor, name: str) -> tuple:
+    if x.dim() != 2:
+        raise ValueError(f"{name} must have two dimensions, got shape {list(x.shape)}")
+    return x.shape
+
+
+def quantize_fp8(x: torch.Tensor, block_rows: int = 1, scale_dtype: torch.dtype = torch.float32, out=None):
+    """x [rows, cols] (fp32 or bf16) -> (q [rows, fp8_ld(cols)] e4m3, scale), one
+    scale per block_rows x 128 elements: 1 for rows of x, 128 for weights
+    [n, k].  out: a (q, scale) pair to write to, whose scale's dtype then counts."""
+    rows, cols = _two_dims(x, "x")
+    if block_rows not in (1, FP8_BLOCK):
+        raise ValueError(f"block_rows must be 1 or {FP8_BLOCK}")
+    q, scale, _ = _fp8_io(x, rows, cols, block_rows, scale_dtype, out)
+    _check(raw().cats_quantize_fp8(x.data_ptr(), _wdtype(x.dtype), rows, cols, block_rows, _SCALE_TYPES[scale.dtype],
+                                   q.data_ptr(), scale.data_ptr(), _stream()))
+    return q, scale
+
+
+def rmsnorm_fp8(x: torch.Tensor, residual: Optional[torch.Tensor] = None, gain: Optional[torch.Tensor] = None,
+                eps: float = 1e-5, scale_dtype: torch.dtype = torch.float32, out=None,
+                sum_out: Optional[torch.Tensor] = None):
+    """(q, scale) of gain * s / sqrt(mean(s^2) + eps), s = x + residual, x [N, d]
+    fp32 or bf16, residual and sum_out [N, d] fp32 (sum_out receives s and may be
+    the residual, or x if fp32), gain [d] fp32; a scale per row and 128 columns."""
+    N, d = _two_dims(x, "x")
+    q, scale, device = _fp8_io(x, N, d, 1, scale_dtype, out)
+    for name, t, shape in (("residual", residual, (N, d)), ("gain", gain, (d,)), ("sum_out", sum_out, (N, d))):
+        if t is not None:
+            _shape_is(t, shape, name)
+            _here(name, t, torch.float32, device)
+    _check(raw().cats_rmsnorm_fp8(x.data_ptr(), _wdtype(x.dtype), _ptr(residual), _ptr(gain), N, d, eps,
+                                  _SCALE_TYPES[scale.dtype], _ptr(sum_out), q.data_ptr(), scale.data_ptr(), _stream()))
+    return q, scale
+
+
+def silu_mul_fp8(gate_up: torch.Tensor, t: float = 0.0, scale_dtype: torch.dtype = torch.float32, out=None):
+    """(q, scale) of h = v u where |v| >= t, else 0, v = SiLU(g), for gate_up
+    [N, 2 m] (a row's gate values, then its up values; fp32 or bf16); a scale
+    per row and 128 neurons."""
+    N, two_m = _two_dims(gate_up, "gate_up")
+    if two_m % 2:
+        raise ValueError(f"gate_up must be [N, 2 m], has {two_m} columns")
+    m = two_m // 2
+    q, scale, _ = _fp8_io(gate_up, N, m, 1, scale_dtype, out)
+    _check(raw().cats_silu_mul_fp8(gate_up.data_ptr(), _wdtype(gate_up.dtype), N, m, t, _SCALE_TYPES[scale.dtype],
+                                   q.data_ptr(), scale.data_ptr(), _stream()))
+    return q, scale
+
+
+def linear_fp8_workspace(N: int, n: int, k: int, device="cuda") -> torch.Tensor:
+    nbytes = int(raw().cats_linear_fp8_workspace_bytes(N, n, k))
+    if nbytes == 0:
+        raise ValueError("arguments outside the supported range")
+    return torch.empty(nbytes, dtype=torch.uint8, device=device)
+
+
+def linear_fp8(xq: torch.Tensor, xs: torch.Tensor, wq: torch.Tensor, wscale: torch.Tensor,
+               residual: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+               dtype: torch.dtype = torch.float32, ws: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """y = residual + x W^T for the rows (xq, xs) and the weight (wq, wscale), both
+    as the quantising calls write them: xq [N, ld], wq [n, ld].  y [N, n] is fp32
+    or bf16 (`dtype`, or out's), the residual of y's type; out may be the residual."""
+    N, ld = _two_dims(xq, "xq")
+    n, ldw = _two_dims(wq, "wq")
+    if ld != ldw or ld % FP8_BLOCK:
+        raise ValueError(f"xq and wq must have the same width, a multiple of {FP8_BLOCK}: got {ld} and {ldw}")
+    _shape_is(xs, (N, ld // FP8_BLOCK), "xs")
+    _shape_is(wscale, (_blocks(n), ld // FP8_BLOCK), "wscale")
+    st = _stype(xs.dtype)
+    if out is not None:
+        _shape_is(out, (N, n), "out")
+        dtype = out.dtype
+    yt = _wdtype(dtype)
+    if residual is not None:
+        _shape_is(residual, (N, n), "residual")
+    if not xq.is_cuda:
+        raise ValueError("xq must be a device tensor")
+    if out is None:
+        out = torch.empty((N, n), dtype=dtype, device=xq.device)
+    device = _device()
+    _here("xq", xq, torch.float8_e4m3fn, device)
+    _here("xs", xs, xs.dtype, device)
+    _here("wq", wq, torch.float8_e4m3fn, device)
+    _here("wscale", wscale, xs.dtype, device)
+    _here("out", out, dtype, device)
+    if residual is not None:
+        _here("residual", residual, dtype, device)
+    if ws is None:
+        ws = linear_fp8_workspace(N, n, ld, device=xq.device)
+    else:
+        _here("ws", ws, torch.uint8, device)
+    _check(raw().cats_linear_fp8(xq.data_ptr(), xs.data_ptr(), N, wq.data_ptr(), wscale.data_ptr(), n, ld, st,
+                                 _ptr(residual), out.data_ptr(), yt, ws.data_ptr(), ws.numel(), _stream()))
     return out
 
 

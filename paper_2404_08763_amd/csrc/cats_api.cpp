@@ -453,6 +453,7 @@ cats::RowsGemmArgs gate_rows(const cats_layer* L, const uint16_t* xs, int N, flo
 
 namespace cats {
 cats_status report_error(cats_status st, const char* msg) { return fail(st, "%s", msg); }
+cats_status enqueued(void* stream, const char* what) { return sync_check(stream, what); }
 }  // namespace cats
 
 static_assert(CATS_MAX_M == cats::kMaxNeurons, "CATS_MAX_M must match the kernel's neuron capacity");

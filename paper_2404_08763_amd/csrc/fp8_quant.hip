@@ -1,0 +1,206 @@
+// The kernels that write 8-bit rows: quantisation alone, RMSNorm with the
+// residual's addition, and the SiLU gate with the CATS cutoff.
+//
+// A scale covers 128 columns: 16 lanes of eight columns, one DPP row, so a
+// block's largest magnitude is four DPP steps away and no value leaves its
+// lane's registers between the load and the 8-byte store of its e4m3 values.
+// All of them are bound by memory: each input is read once and each output
+// written once.
+#include "fp8.hpp"
+#include "internal.hpp"
+
+namespace cats {
+
+// Stores eight values of block (row, cb) and, from the group's first lane, its scale.
+template <bool E8M0>
+__device__ __forceinline__ void put_block(const Fp8Out& o, size_t row, int cb, int sub, uint32_t amax,
+                                          const float (&f)[8]) {
+  float inv;
+  const typename Fp8Scale<E8M0>::type s = Fp8Scale<E8M0>::stored(amax, inv);
+  const uint2 v = {fp8x4(f, inv), fp8x4(f + 4, inv)};
+  *reinterpret_cast<uint2*>(o.q + row * o.ld + (size_t)cb * kFp8Block + sub * 8) = v;
+  if (sub == 0) reinterpret_cast<typename Fp8Scale<E8M0>::type*>(o.scale)[row * (o.ld / kFp8Block) + cb] = s;
+}
+
+// One group of 16 lanes per block of 128 columns of a row.  GATE: the row
+// holds m gate values, then m up values; h = SiLU(g) u where |SiLU(g)| is not below t.
+template <typename T, bool E8M0, bool GATE>
+__global__ __launch_bounds__(256) void k_fp8_rows(const T* __restrict__ x, int cols, float t, uint32_t blocks, Fp8Out o) {
+  const uint32_t b = blockIdx.x * 16u + threadIdx.x / 16u;
+  if (b >= blocks) return;
+  const uint32_t nb = (uint32_t)o.ld / kFp8Block, row = b / nb;
+  const int cb = (int)(b - row * nb), sub = threadIdx.x & 15, c = cb * kFp8Block + sub * 8;
+  const T* xr = x + (size_t)row * cols * (GATE ? 2 : 1);
+  float f[8];
+  load8(xr, c, cols, f);
+  if constexpr (GATE) {
+    float u[8];
+    load8(xr + cols, c, cols, u);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float v = silu(f[e]);
+      f[e] = fabsf(v) < t ? 0.f : v * u[e];
+    }
+  }
+  put_block<E8M0>(o, row, cb, sub, max16(finite_max8(f)), f);
+}
+
+// One block of 256 threads per 128 x 128 weights, 64 of them per thread.
+template <typename T, bool E8M0>
+__global__ __launch_bounds__(256) void k_fp8_tiles(const T* __restrict__ x, int rows, int cols, Fp8Out o) {
+  __shared__ uint32_t red[16];
+  const int nb = o.ld / kFp8Block;
+  const int rb = blockIdx.x / nb, cb = blockIdx.x - rb * nb;
+  const int grp = threadIdx.x / 16, sub = threadIdx.x & 15, c = cb * kFp8Block + sub * 8;
+  const int r0 = rb * kFp8Block + grp;
+  float f[8][8];
+  uint32_t a = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int r = r0 + 16 * i;
+    if (r < rows) {
+      load8(x + (size_t)r * cols, c, cols, f[i]);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) f[i][e] = 0.f;
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) a = max(a, finite_max8(f[i]));
+  a = max16(a);
+  if (sub == 0) red[grp] = a;
+  __syncthreads();
+  a = max16(red[sub]);
+  float inv;
+  const typename Fp8Scale<E8M0>::type s = Fp8Scale<E8M0>::stored(a, inv);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int r = r0 + 16 * i;
+    if (r < rows)
+      *reinterpret_cast<uint2*>(o.q + (size_t)r * o.ld + c) = uint2{fp8x4(f[i], inv), fp8x4(f[i] + 4, inv)};
+  }
+  if (threadIdx.x == 0) reinterpret_cast<typename Fp8Scale<E8M0>::type*>(o.scale)[(size_t)rb * nb + cb] = s;
+}
+
+// One block per row, the row in registers (NV chunks of eight columns per thread):
+// one read of x and the residual.
+template <typename T, bool E8M0, int NV>
+__global__ __launch_bounds__(1024) void k_rmsnorm_fp8(RmsnormFp8Args a) {
+  __shared__ float red[16];
+  const int d = a.d, tid = threadIdx.x, T0 = blockDim.x;
+  const size_t row = blockIdx.x;
+  const T* xr = static_cast<const T*>(a.x) + row * d;
+  float f[NV][8];
+  float ss = 0.f;
+#pragma unroll
+  for (int i = 0; i < NV; ++i) load8(xr, (tid + T0 * i) * 8, d, f[i]);
+  if (a.residual) {
+    float r[NV][8];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) load8(a.residual + row * d, (tid + T0 * i) * 8, d, r[i]);
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) f[i][e] += r[i][e];
+  }
+  if (a.sum) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) store8(a.sum + row * d, (tid + T0 * i) * 8, d, f[i]);
+  }
+#pragma unroll
+  for (int i = 0; i < NV; ++i)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) ss = fmaf(f[i][e], f[i][e], ss);
+  ss = wave_sum(ss);
+  const int nw = T0 / kWaveSize;
+  if (nw > 1) {
+    if ((tid & (kWaveSize - 1)) == 0) red[tid / kWaveSize] = ss;
+    __syncthreads();
+    ss = red[0];
+    for (int w = 1; w < nw; ++w) ss += red[w];
+  }
+  const float inv = 1.0f / sqrtf(ss / (float)d + a.eps);
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const int c = (tid + T0 * i) * 8;
+    if (c >= a.o.ld) continue;
+    float y[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) y[e] = f[i][e] * inv;
+    if (a.gain) {
+      float g[8];
+      load8(a.gain, c, d, g);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) y[e] *= g[e];
+    }
+    put_block<E8M0>(a.o, row, c / kFp8Block, (c / 8) & 15, max16(finite_max8(y)), y);
+  }
+}
+
+namespace {
+template <typename T, bool GATE>
+hipError_t rows_launch(const char* name, const void* x, int N, int cols, float t, const Fp8Out& o, hipStream_t s) {
+  const uint32_t blocks = (uint32_t)N * (uint32_t)(o.ld / kFp8Block);
+  const dim3 grid((blocks + 15) / 16);
+  KernelTimer timer(name, s);
+  if (o.e8m0)
+    hipExtLaunchKernelGGL((k_fp8_rows<T, true, GATE>), grid, dim3(256), 0, s, timer.start(), timer.stop(), 0,
+                          static_cast<const T*>(x), cols, t, blocks, o);
+  else
+    hipExtLaunchKernelGGL((k_fp8_rows<T, false, GATE>), grid, dim3(256), 0, s, timer.start(), timer.stop(), 0,
+                          static_cast<const T*>(x), cols, t, blocks, o);
+  return hipGetLastError();
+}
+
+template <typename T>
+hipError_t tiles_launch(const void* x, int rows, int cols, const Fp8Out& o, hipStream_t s) {
+  const dim3 grid((unsigned)((rows + kFp8Block - 1) / kFp8Block) * (unsigned)(o.ld / kFp8Block));
+  KernelTimer timer("quantize_fp8_tiles", s);
+  if (o.e8m0)
+    hipExtLaunchKernelGGL((k_fp8_tiles<T, true>), grid, dim3(256), 0, s, timer.start(), timer.stop(), 0,
+                          static_cast<const T*>(x), rows, cols, o);
+  else
+    hipExtLaunchKernelGGL((k_fp8_tiles<T, false>), grid, dim3(256), 0, s, timer.start(), timer.stop(), 0,
+                          static_cast<const T*>(x), rows, cols, o);
+  return hipGetLastError();
+}
+
+template <typename T, bool E8M0, int NV>
+hipError_t norm_launch_nv(const RmsnormFp8Args& a, int threads, hipStream_t s) {
+  KernelTimer timer("rmsnorm_fp8", s);
+  hipExtLaunchKernelGGL((k_rmsnorm_fp8<T, E8M0, NV>), dim3(a.N), dim3(threads), 0, s, timer.start(), timer.stop(), 0, a);
+  return hipGetLastError();
+}
+
+template <typename T, bool E8M0>
+hipError_t norm_launch(const RmsnormFp8Args& a, hipStream_t s) {
+  const int chunks = a.o.ld / 8;
+  const int nv = chunks <= 1024 ? 1 : chunks <= 2048 ? 2 : chunks <= 4096 ? 4 : 8;
+  const int threads = ((chunks + nv - 1) / nv + kWaveSize - 1) / kWaveSize * kWaveSize;
+  switch (nv) {
+    case 1: return norm_launch_nv<T, E8M0, 1>(a, threads, s);
+    case 2: return norm_launch_nv<T, E8M0, 2>(a, threads, s);
+    case 4: return norm_launch_nv<T, E8M0, 4>(a, threads, s);
+    default: return norm_launch_nv<T, E8M0, 8>(a, threads, s);
+  }
+}
+}  // namespace
+
+hipError_t launch_quantize_fp8(const void* x, int bf16, int rows, int cols, int block_rows, const Fp8Out& o, hipStream_t s) {
+  if (block_rows == 1)
+    return bf16 ? rows_launch<uint16_t, false>("quantize_fp8_rows", x, rows, cols, 0.f, o, s)
+                : rows_launch<float, false>("quantize_fp8_rows", x, rows, cols, 0.f, o, s);
+  return bf16 ? tiles_launch<uint16_t>(x, rows, cols, o, s) : tiles_launch<float>(x, rows, cols, o, s);
+}
+
+hipError_t launch_silu_fp8(const void* gu, int bf16, int N, int m, float t, const Fp8Out& o, hipStream_t s) {
+  return bf16 ? rows_launch<uint16_t, true>("silu_mul_fp8", gu, N, m, t, o, s)
+              : rows_launch<float, true>("silu_mul_fp8", gu, N, m, t, o, s);
+}
+
+hipError_t launch_rmsnorm_fp8(const RmsnormFp8Args& a, int bf16, hipStream_t s) {
+  if (bf16) return a.o.e8m0 ? norm_launch<uint16_t, true>(a, s) : norm_launch<uint16_t, false>(a, s);
+  return a.o.e8m0 ? norm_launch<float, true>(a, s) : norm_launch<float, false>(a, s);
+}
+
+}  // namespace cats

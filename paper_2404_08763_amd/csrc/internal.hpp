@@ -7,9 +7,16 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include "cats.h"
 #include "fused_params.hpp"
 
 namespace cats {
+
+// Records the message of a failed call on this thread and returns its status.
+cats_status report_error(cats_status st, const char* msg);
+// What an enqueue-only call returns once its launches are out: CATS_OK, or with
+// CATS_SYNC_CHECK set the status of the synchronised stream.
+cats_status enqueued(void* stream, const char* what);
 
 constexpr int kDownCols = 512;  // columns of a down-projection block
 
@@ -228,6 +235,38 @@ hipError_t launch_stream_read(const void* buf, uint32_t bytes, int blocks, int i
                               hipStream_t s);
 hipError_t launch_transpose(const void* in, void* out, int rows, int cols, int elem_bytes,
                             hipStream_t s);
+
+// 8-bit rows and weights (fp8_quant.hip, fp8_linear.hip): e4m3 values
+// [rows x ld] and the scales of their blocks of 128 columns.
+struct Fp8Out {
+  uint8_t* q;
+  void* scale;  // fp32, or E8M0 bytes
+  int ld;
+  int e8m0;
+};
+struct RmsnormFp8Args {
+  const void* x;          // [N x d] fp32 or bf16
+  const float* residual;  // [N x d] or null
+  const float* gain;      // [d] or null
+  float* sum;             // [N x d] or null; may be residual or x
+  int N, d;
+  float eps;
+  Fp8Out o;
+};
+struct LinearFp8Args {
+  const uint8_t* xq;     // [N x ld]
+  const void* xs;        // [N x ld / 128]
+  const uint8_t* wq;     // [n x ld]
+  const void* ws;        // [ceil(n / 128) x ld / 128]
+  const void* residual;  // [N x n] of y's type, or null; may be y
+  void* y;               // [N x n] fp32 or bf16
+  int N, n, ld;
+  int e8m0, ybf16;
+};
+hipError_t launch_quantize_fp8(const void* x, int bf16, int rows, int cols, int block_rows, const Fp8Out& o, hipStream_t s);
+hipError_t launch_silu_fp8(const void* gu, int bf16, int N, int m, float t, const Fp8Out& o, hipStream_t s);
+hipError_t launch_rmsnorm_fp8(const RmsnormFp8Args& a, int bf16, hipStream_t s);
+hipError_t launch_linear_fp8(const LinearFp8Args& a, hipStream_t s);
 
 // Optional per-kernel timing (cats_timer_*): while the timer is enabled a
 // KernelTimer hands out a pair of HIP events that the launch (through

@@ -1,0 +1,405 @@
+"""The 8-bit operators on the device against their 64-bit definitions."""
+import pytest
+import torch
+
+import paper_2404_08763_amd as P
+from paper_2404_08763_amd import workloads as W
+
+from fp8_util import BLOCK, E8M0, F32, U, check_linear, check_quantised, gen, ld_of, linear_ref, quantised
+from gpu_util import say
+
+pytestmark = pytest.mark.gpu
+
+SCALES = [F32, E8M0]
+IDS = ["f32", "e8m0"]
+DEV = "cuda"
+
+
+def _same(a, b):
+    return torch.equal(a.contiguous().view(torch.uint8), b.contiguous().view(torch.uint8))
+
+
+def _rows(N, d, seed, dtype=torch.float32):
+    x = torch.randn((N, d), generator=gen(seed))
+    x[:, :: 97] *= 20.0
+    return x.to(dtype).to(DEV)
+
+
+# ---- quantisation ------------------------------------------------------------
+
+@pytest.mark.parametrize("stype", SCALES, ids=IDS)
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["x32", "x16"])
+@pytest.mark.parametrize("up", [1, 128])
+@pytest.mark.parametrize("rows,cols", [(1, 1), (1, 128), (3, 127), (5, 129), (127, 8), (128, 256), (129, 1001), (300, 4096)])
+def test_quantize(rows, cols, up, dtype, stype):
+    say("quantize", rows, cols, up, dtype, stype)
+    x = _rows(rows, cols, rows + cols, dtype)
+    q, s = P.quantize_fp8(x, block_rows=up, scale_dtype=stype)
+    check_quantised(x, q, s, up, 0.0)
+
+
+@pytest.mark.parametrize("stype", SCALES, ids=IDS)
+@pytest.mark.parametrize("up", [1, 128])
+def test_quantize_special_values(up, stype):
+    """Zeros, tiny and huge blocks, infinities and NaN; largest values at and next to 448 2^e."""
+    say("quantize special", up, stype)
+    top = torch.finfo(torch.float32).max
+    x = torch.randn((256, 1100), generator=gen(3))
+    for r in (0, 128):  # (in both row blocks)
+        x[r:r + 128, 0:128] = 0.0
+        x[r:r + 128, 128:256] *= 1e-42       # below the least scale
+        x[r:r + 128, 256:384] *= 1e-38
+        x[r:r + 128, 384:512] *= top / 8
+        x[r + 5, 512:516] = torch.tensor([float("inf"), -float("inf"), float("nan"), 1e-3])
+        x[r:r + 128, 640:768] = float("nan")
+        x[r:r + 128, 768:896] = x[r:r + 128, 768:896].clamp(-3, 3)
+        x[r + 7, 800] = 448.0 * 2.0 ** -6    # = 7: just fits 2^-6
+        x[r:r + 128, 896:1024] = x[r:r + 128, 896:1024].clamp(-3, 3)
+        x[r + 7, 900] = -7.000001
+    x[0, 384] = top
+    q, s = P.quantize_fp8(x.to(DEV), block_rows=up, scale_dtype=stype)
+    check_quantised(x, q, s, up, 0.0)
+
+
+def test_quantize_reads_unaligned_rows():
+    """A view that starts at an odd element, rows of an odd width."""
+    say("quantize unaligned")
+    base = torch.randn(1 + 7 * 131, generator=gen(5)).to(DEV)
+    for dtype in (torch.float32, torch.bfloat16):
+        x = base.to(dtype)[1:].view(7, 131)
+        q, s = P.quantize_fp8(x)
+        check_quantised(x, q, s, 1, 0.0)
+
+
+# ---- RMSNorm -------------------------------------------------------------------
+
+# mean of d squares in fp32 with at most 64 + 6 + 16 additions in a chain, half of
+# that through the root; the quotient, the root, its use and the gain 5 roundings
+NORM_DELTA = 64 * U
+
+
+def _norm_ref(x, residual, gain, eps):
+    s = x.double() + (residual.double() if residual is not None else 0.0)
+    s32 = s.float().double()  # the sum as the device holds it
+    y = s32 / torch.sqrt(s32.square().mean(dim=1, keepdim=True) + eps)
+    return s, y * gain.double() if gain is not None else y
+
+
+@pytest.mark.parametrize("stype", SCALES, ids=IDS)
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["x32", "x16"])
+@pytest.mark.parametrize("res,gain", [(False, False), (True, True), (True, False)])
+@pytest.mark.parametrize("N,d", [(1, 1), (2, 127), (3, 128), (1, 4096), (17, 2856), (5, 5121), (3, 8192), (2, 16385),
+                                 (2, 32768), (1, 65535)])
+def test_rmsnorm(N, d, res, gain, dtype, stype):
+    say("rmsnorm", N, d, res, gain, dtype, stype)
+    x = _rows(N, d, 7 * N + d, dtype)
+    r = torch.randn((N, d), generator=gen(1)).to(DEV) if res else None
+    g = (1 + 0.1 * torch.randn(d, generator=gen(2))).to(DEV) if gain else None
+    total = torch.full((N, d), float("nan"), device=DEV)
+    q, s = P.rmsnorm_fp8(x, residual=r, gain=g, eps=1e-5, scale_dtype=stype, sum_out=total)
+    want, y = _norm_ref(x, r, g, 1e-5)
+    assert torch.equal(total, want.float()), "one rounding of an exact sum"
+    check_quantised(y, q, s, 1, NORM_DELTA)
+    if res:  # the residual stream in place
+        q2, s2 = P.rmsnorm_fp8(x, residual=r, gain=g, eps=1e-5, scale_dtype=stype, sum_out=r)
+        assert torch.equal(r, total) and _same(q, q2) and _same(s, s2)
+
+
+def test_rmsnorm_special_rows():
+    """Rows of zeros, a NaN, an infinity, a huge and a tiny row beside ordinary ones."""
+    say("rmsnorm special")
+    x = torch.randn((6, 300), generator=gen(4))
+    x[1] = 0.0
+    x[2, 17] = float("nan")
+    x[3, 40] = float("inf")
+    x[4] *= 1e30   # the squares overflow: zeros, as cats_rmsnorm
+    x[5] *= 1e-30
+    for eps in (1e-5, 0.0):
+        q, s = P.rmsnorm_fp8(x.to(DEV), eps=eps)
+        plain = P.rmsnorm(x.to(DEV), eps=eps).cpu()
+        qf = q.float().cpu()[:, :300]
+        assert torch.equal(torch.isnan(qf), ~torch.isfinite(plain))  # (eps = 0: zero and tiny rows divide by 0)
+        assert (qf[3, :40] == 0).all() and (qf[4] == 0).all()
+        ok = [0, 1, 5] if eps else [0]
+        check_quantised(plain[ok], q[ok], s[ok], 1, NORM_DELTA)
+
+
+# ---- gate ------------------------------------------------------------------------
+
+# e^-z in fp32 with |z| <= 20: 20 * 1.5 + 4 half steps; the sum, quotient and product 4
+GATE_DELTA = 40 * U
+
+
+@pytest.mark.parametrize("stype", SCALES, ids=IDS)
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["x32", "x16"])
+@pytest.mark.parametrize("t", [0.0, 0.15, float("inf")])
+@pytest.mark.parametrize("N,m", [(1, 1), (1, 128), (2, 129), (33, 1001), (3, 11008), (100, 2000)])
+def test_silu_mul(N, m, t, dtype, stype):
+    say("gate", N, m, t, dtype, stype)
+    gu = (1.3 * torch.randn((N, 2 * m), generator=gen(N + m))).to(dtype).to(DEV)
+    q, s = P.silu_mul_fp8(gu, t=t, scale_dtype=stype)
+    g, u = gu[:, :m].double(), gu[:, m:].double()
+    v = g * torch.sigmoid(g)
+    t32 = float(torch.tensor(t, dtype=torch.float32))
+    border = (v.abs() - t32).abs() <= GATE_DELTA * v.abs() if t32 < float("inf") and t32 > 0 else torch.zeros_like(v, dtype=torch.bool)
+    h = torch.where((v.abs() < t32) & ~border, torch.zeros_like(v), v * u)
+    check_quantised(h, q, s, 1, GATE_DELTA, drop=border.cpu())
+    if t == float("inf"):
+        assert (q.float() == 0).all() and (s.float() == 1).all()
+
+
+def test_silu_mul_special_values():
+    say("gate special")
+    g = torch.tensor([[0.0, -200.0, 200.0, float("nan"), float("inf"), -0.5, 0.2, -90.0]])
+    u = torch.tensor([[3.0, 2.0, 0.5, 1.0, 1.0, float("nan"), float("inf"), 1.0]])
+    q, s = P.silu_mul_fp8(torch.cat([g, u], dim=1).to(DEV), t=0.15)
+    qf = q.float().cpu()[0]
+    # v: 0 and -0 masked; 200 kept; NaN kept; inf; |-0.189| kept, times NaN; |0.11| masked, whatever u is; -0
+    assert qf[[0, 1, 6, 7]].tolist() == [0, 0, 0, 0]
+    assert torch.isnan(qf[[3, 4, 5]]).all()
+    assert float(qf[2]) == 448.0 and abs(float(s[0, 0]) * 448.0 - 100.0) < 1e-4
+
+
+# ---- linear --------------------------------------------------------------------------
+
+def _operands(N, n, k, stype, seed=0):
+    x = _rows(N, k, 11 + seed)
+    w = 0.02 * torch.randn((n, k), generator=gen(13 + seed, DEV), device=DEV)
+    return quantised(x, 1, stype) + quantised(w, BLOCK, stype)
+
+
+LINEAR = [(1, 1, 1), (1, 16, 128), (1, 6144, 4096), (2, 130, 129), (5, 40, 7001), (16, 257, 512), (17, 129, 1000), (31, 2000, 257),
+          (33, 257, 384), (48, 1000, 3000), (64, 512, 2048), (65, 4096, 640), (100, 300, 2000), (128, 513, 1152),
+          (129, 4097, 128), (255, 640, 4096), (257, 1000, 4224), (300, 2048, 8320), (512, 1024, 256), (700, 3001, 1000),
+          (1024, 2048, 384), (2000, 4100, 300)]
+
+
+@pytest.mark.parametrize("stype", SCALES, ids=IDS)
+@pytest.mark.parametrize("N,n,k", LINEAR)
+def test_linear(N, n, k, stype):
+    say("linear", N, n, k, stype)
+    xq, xs, wq, ws = _operands(N, n, k, stype)
+    r = torch.randn((N, n), generator=gen(9)).to(DEV)
+    ref, mag = linear_ref(xq, xs, wq, ws)
+    ld = ld_of(k)
+    out = torch.full((N, n), float("nan"), device=DEV)
+    y = P.linear_fp8(xq, xs, wq, ws, out=out)
+    assert y is out
+    check_linear(y, ref, mag, ld)
+    y16 = P.linear_fp8(xq, xs, wq, ws, dtype=torch.bfloat16)
+    check_linear(y16, ref, mag, ld)
+    yr = P.linear_fp8(xq, xs, wq, ws, residual=r)
+    check_linear(yr, ref + r.double(), mag + r.double().abs(), ld)
+    r16 = r.bfloat16()
+    want = ref + r16.double()
+    assert P.linear_fp8(xq, xs, wq, ws, residual=r16, out=r16) is r16  # in place
+    check_linear(r16, want, mag + want.abs(), ld)
+    assert _same(P.linear_fp8(xq, xs, wq, ws), y), "bit for bit again"
+
+
+def _guarded(shape, dtype):
+    """A tensor between two stretches of a known pattern, and a check of them."""
+    count = 1
+    for v in shape:
+        count *= v
+    size = torch.empty((), dtype=dtype).element_size()
+    whole = torch.full((count * size + 8192,), 0x5a, dtype=torch.uint8, device=DEV)
+    inner = whole[4096:4096 + count * size]
+    return inner.view(dtype).view(shape), lambda: bool((whole[:4096] == 0x5a).all() and (whole[4096 + count * size:] == 0x5a).all())
+
+
+@pytest.mark.parametrize("stype", SCALES, ids=IDS)
+@pytest.mark.parametrize("N,n,k", [(1, 33, 200), (19, 130, 128), (130, 259, 500), (300, 513, 1000)])
+def test_writes_stay_inside(N, n, k, stype):
+    say("guards", N, n, k, stype)
+    xq, xs, wq, ws = _operands(N, n, k, stype)
+    y, ok = _guarded((N, n), torch.float32)
+    P.linear_fp8(xq, xs, wq, ws, out=y)
+    assert ok()
+    need = P.linear_fp8_workspace(N, n, ld_of(k)).numel()
+    scratch, ok_ws = _guarded((need,), torch.uint8)
+    P.linear_fp8(xq, xs, wq, ws, out=y, ws=scratch)
+    assert ok() and ok_ws()
+    q, ok_q = _guarded((N, ld_of(k)), torch.float8_e4m3fn)
+    s, ok_s = _guarded((N, ld_of(k) // BLOCK), stype)
+    x = _rows(N, k, 1)
+    P.quantize_fp8(x, out=(q, s))
+    assert ok_q() and ok_s()
+    total, ok_t = _guarded((N, k), torch.float32)
+    P.rmsnorm_fp8(x, residual=x.clone(), sum_out=total, out=(q, s))
+    assert ok_q() and ok_s() and ok_t()
+    P.silu_mul_fp8(_rows(N, 2 * k, 2), t=0.1, out=(q, s))
+    assert ok_q() and ok_s()
+    wq2, ok_q = _guarded((n, ld_of(k)), torch.float8_e4m3fn)
+    ws2, ok_s = _guarded(((n + 127) // 128, ld_of(k) // BLOCK), stype)
+    P.quantize_fp8(_rows(n, k, 3), block_rows=128, out=(wq2, ws2))
+    assert ok_q() and ok_s()
+
+
+@pytest.mark.parametrize("N", [1, 40, 300])
+def test_linear_any_fp32_scale(N):
+    """Scales a user brings: negative, zero, any; a NaN or infinite scale reaches its rows alone."""
+    say("linear scales", N)
+    xq, xs, wq, ws = _operands(N, 300, 512, F32)
+    xs = xs * torch.randn(xs.shape, generator=gen(1)).to(DEV)
+    ws = ws * torch.randn(ws.shape, generator=gen(2)).to(DEV)
+    xs[:, 1] = 0.0
+    ref, mag = linear_ref(xq, xs, wq, ws)
+    check_linear(P.linear_fp8(xq, xs, wq, ws), ref, mag, 512)
+    xs[N - 1, 2] = float("nan")
+    ws[1, 0] = float("inf")
+    y = P.linear_fp8(xq, xs, wq, ws)
+    assert torch.isnan(y[N - 1]).all()
+    assert not torch.isfinite(y[:, 128:256]).any()
+    if N > 1:
+        check_linear(y[:-1, :128], ref[:-1, :128], mag[:-1, :128], 512)
+        check_linear(y[:-1, 256:], ref[:-1, 256:], mag[:-1, 256:], 512)
+
+
+@pytest.mark.parametrize("N", [1, 40, 300])
+def test_linear_e8m0_range(N):
+    """Scales whose product is ordinary though each is extreme, and a NaN scale."""
+    say("linear e8m0", N)
+    xq, xs, wq, ws = _operands(N, 200, 384, E8M0)
+    xs.view(torch.uint8)[:, 0] = 0      # 2^-127
+    ws.view(torch.uint8)[:, 0] = 254    # 2^127
+    xs.view(torch.uint8)[:, 2] = 240
+    ws.view(torch.uint8)[:, 2] = 10
+    ref, mag = linear_ref(xq, xs, wq, ws)
+    check_linear(P.linear_fp8(xq, xs, wq, ws), ref, mag, 384)
+    xs.view(torch.uint8)[0, 1] = 255
+    y = P.linear_fp8(xq, xs, wq, ws)
+    assert torch.isnan(y[0]).all()
+    if N > 1:
+        check_linear(y[1:], ref[1:], mag[1:], 384)
+
+
+@pytest.mark.parametrize("stype", SCALES, ids=IDS)
+@pytest.mark.parametrize("N", [3, 50, 260])
+def test_linear_nan_in_q_stays_in_its_row(N, stype):
+    say("linear nan", N, stype)
+    xq, xs, wq, ws = _operands(N, 140, 640, stype)
+    ref, mag = linear_ref(xq, xs, wq, ws)
+    xq.view(torch.uint8)[1, 600] = 0x7f
+    wq.view(torch.uint8)[139, 0] = 0xff
+    y = P.linear_fp8(xq, xs, wq, ws)
+    assert torch.isnan(y[1]).all() and torch.isnan(y[:, 139]).all()
+    keep = [i for i in range(N) if i != 1]
+    check_linear(y[keep][:, :139], ref[keep][:, :139], mag[keep][:, :139], 640)
+
+
+# ---- together --------------------------------------------------------------------------
+
+def _block(stype, c, seed=0):
+    """A gated-MLP block's 8-bit weights from its math-layout ones."""
+    wg, wu, wd = W.weights(c[0], c[1], torch.bfloat16, layer=seed)
+    layer = P.layer_from_math(wg.cuda(), wu.cuda(), wd.cuda())
+    gu = torch.cat([layer.w_gate_t, layer.w_up_t])
+    down = P.pack_weights(layer.w_down)
+    return layer, P.quantize_fp8(gu, 128, stype), P.quantize_fp8(down, 128, stype)
+
+
+def _mlp(x, gu, down, t, stype, dtype=torch.float32):
+    """x + MLP(RMSNorm(x)) on 8-bit operands."""
+    xn = P.rmsnorm_fp8(x, scale_dtype=stype)
+    g = P.linear_fp8(*xn, *gu, dtype=dtype)
+    h = P.silu_mul_fp8(g, t=t, scale_dtype=stype)
+    return P.linear_fp8(*h, *down, residual=x), xn, g, h
+
+
+@pytest.mark.parametrize("stype", SCALES, ids=IDS)
+@pytest.mark.parametrize("N,d,m", [(1, 512, 1376), (16, 256, 693), (200, 512, 1376)])
+def test_block_against_dense_and_step_by_step(N, d, m, stype):
+    say("block", N, d, m, stype)
+    layer, gu, down = _block(stype, (d, m))
+    x = _rows(N, d, 21)
+    y, xn, g, h = _mlp(x, gu, down, 0.0, stype)
+    # each step against its definition on the step's own inputs
+    ref, mag = linear_ref(*xn, *gu)
+    check_linear(g, ref, mag, ld_of(d))
+    v = g[:, :m].double()
+    check_quantised(v * torch.sigmoid(v) * g[:, m:].double(), *h, 1, GATE_DELTA)
+    ref, mag = linear_ref(*h, *down, residual=x)
+    check_linear(y, ref, mag, ld_of(m))
+    # the whole against the dense block on bf16 weights.  An e4m3 value is off by at
+    # most 2^-4 and 0.026 in the mean square (uniform over a step, averaged
+    # over a binade), so a product of two of them by 0.037; gate, up and down
+    # products and h's own rounding: 0.037 sqrt(3) and 0.026, the gate's error
+    # enlarged by up to 1.5 through SiLU: under 0.12 of the block's output
+    dense = torch.cat([P.mlp_dense(layer, P.rmsnorm(x[i:i + 16].contiguous())) for i in range(0, N, 16)])
+    err = (y - x - dense).double()
+    assert float(err.norm()) <= 0.12 * float(dense.double().norm())
+
+
+def test_block_with_cutoff_drops_what_the_forward_drops():
+    say("block cutoff")
+    layer, gu, down = _block(F32, (512, 1376))
+    x = _rows(8, 512, 22)
+    _, _, g, h = _mlp(x, gu, down, 0.1, F32)
+    v = g[:, :1376].double()
+    v = (v * torch.sigmoid(v)).abs()
+    kept = h[0].float()[:, :1376] != 0
+    assert not kept[v < 0.1 * (1 - GATE_DELTA)].any()
+    assert (kept | (v < 0.1 * (1 + GATE_DELTA)) | ((v * g[:, 1376:].abs()) < h[1].repeat_interleave(BLOCK, 1)[:, :1376] * 2.0 ** -9)).all()
+
+
+@pytest.mark.parametrize("N", [1, 24, 300])
+def test_captured_block_replays(N):
+    """A captured block replayed with eager work and synchronisations between, on changing input."""
+    say("graph", N)
+    _, gu, down = _block(E8M0, (256, 640))
+    x = _rows(N, 256, 31)
+    ws = torch.empty(1 << 22, dtype=torch.uint8, device=DEV)
+    qx = (torch.empty((N, 256), dtype=torch.float8_e4m3fn, device=DEV), torch.empty((N, 2), dtype=E8M0, device=DEV))
+    qh = (torch.empty((N, 640), dtype=torch.float8_e4m3fn, device=DEV), torch.empty((N, 5), dtype=E8M0, device=DEV))
+    g = torch.empty((N, 1280), dtype=torch.bfloat16, device=DEV)
+    y = torch.empty((N, 256), device=DEV)
+
+    def call():
+        P.rmsnorm_fp8(x, out=qx)
+        P.linear_fp8(*qx, *gu, out=g, ws=ws)
+        P.silu_mul_fp8(g, t=0.05, out=qh)
+        P.linear_fp8(*qh, *down, residual=x, out=y, ws=ws)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        call()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for i in range(4):
+        x.copy_(_rows(N, 256, 40 + i))
+        want = _mlp(x, gu, down, 0.05, E8M0, torch.bfloat16)[0]
+        torch.cuda.synchronize()
+        y.fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert _same(y, want), i
+
+
+def test_calls_run_on_the_current_stream():
+    say("streams")
+    xq, xs, wq, ws = _operands(40, 300, 512, F32)
+    want = P.linear_fp8(xq, xs, wq, ws)
+    torch.cuda.synchronize()
+    side = [torch.cuda.Stream() for _ in range(2)]
+    outs = []
+    for st in side:  # two calls at once, each with its workspace
+        st.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(st):
+            outs.append([P.linear_fp8(xq, xs, wq, ws) for _ in range(4)])
+    torch.cuda.synchronize()
+    assert all(_same(o, want) for group in outs for o in group)
+
+
+def test_workspace_holds_anything():
+    say("workspace")
+    for N, n, k in ((1, 300, 512), (50, 300, 4096), (300, 200, 8192)):
+        xq, xs, wq, ws = _operands(N, n, k, F32)
+        want = P.linear_fp8(xq, xs, wq, ws)
+        for fill in (0, 1, 255):
+            scratch = P.linear_fp8_workspace(N, n, ld_of(k)).fill_(fill)
+            for _ in range(2):
+                assert _same(P.linear_fp8(xq, xs, wq, ws, ws=scratch), want)
