@@ -141,9 +141,10 @@ __global__ __launch_bounds__(512, 2) void k_fp8_tile(LinearFp8Args a, int MT, in
   constexpr int MI = G::MI, NB = G::NB;
   constexpr int TM = 16 * MI * G::WM, TN = 16 * NB * G::WN;
   constexpr int WQ = TM / 64, XQ = TN / 64;  // loads of a wave and step: 1 KB (8 rows) each
+  constexpr int WB = TM / kFp8Block;         // the weight's scales of a step
   constexpr bool HW = E8M0 && !PREC;         // scales applied by the matrix instruction
   __shared__ __attribute__((aligned(1024))) uint8_t sw0[TM * 128], sx0[TN * 128], sw1[TM * 128], sx1[TN * 128];
-  __shared__ uint32_t ss0[TN], ss1[TN];
+  __shared__ uint32_t ss0[TN + WB], ss1[TN + WB];
   const int tid = threadIdx.x, lane = tid & (kWaveSize - 1);
   const int w = __builtin_amdgcn_readfirstlane(tid / kWaveSize);
   const int wm = w / G::WN, wn = w % G::WN;
@@ -172,29 +173,31 @@ __global__ __launch_bounds__(512, 2) void k_fp8_tile(LinearFp8Args a, int MT, in
 #pragma unroll
     for (int q = 0; q < XQ; ++q) dma16(rx, sx + (XQ * w + q) * 1024, xoff + (k + 8u * q * a.ld));
   };
-  // The scales of a step: one of the weight (a wave's outputs lie in one block of
-  // 128), one of each of the lane's rows.
+  // The scales of a step: each wave of the first group fetches those of 64 of the
+  // tile's rows and one of the weight's into registers and, a phase later, puts them
+  // into LDS (some waves the same).  Not a load where they are used: its wait
+  // would be one for the step's operands too.
   constexpr uint32_t SB = E8M0 ? 1 : 4;
-  const int wsrow = min((c0 + 16 * MI * wm) / kFp8Block, (a.n - 1) / kFp8Block);
-  const uint8_t* wsp = static_cast<const uint8_t*>(a.ws) + (size_t)wsrow * KB * SB;
-  const __amdgpu_buffer_rsrc_t rs =
+  const int wb = min(c0 / kFp8Block + w % WB, (a.n - 1) / kFp8Block), srow = (64 * w + lane) % TN;
+  const __amdgpu_buffer_rsrc_t rsw = make_rsrc(static_cast<const uint8_t*>(a.ws) + (size_t)wb * KB * SB, (uint32_t)KB * SB);
+  const __amdgpu_buffer_rsrc_t rsx =
       make_rsrc(static_cast<const uint8_t*>(a.xs) + (size_t)t0 * KB * SB, (uint32_t)nt * KB * SB);
-  // Each wave of the first group fetches the scales of 64 of the tile's rows
-  // into a register and, a phase later, puts them into LDS.
-  const uint32_t soff = (uint32_t)(64 * w + lane) * KB * SB;
-  uint32_t pend = 0;
+  const uint32_t soff = (uint32_t)srow * KB * SB;
+  uint32_t px = 0, pw = 0;
   auto fetch_scales = [&](int st) {
-    if (64 * w < TN) {
-      if constexpr (E8M0)
-        pend = __builtin_amdgcn_raw_buffer_load_b8(rs, (int)(soff + (uint32_t)st), 0, 0);
-      else
-        pend = __builtin_amdgcn_raw_buffer_load_b32(rs, (int)(soff + (uint32_t)st * 4u), 0, 0);
+    if constexpr (E8M0) {
+      px = __builtin_amdgcn_raw_buffer_load_b8(rsx, (int)(soff + (uint32_t)st), 0, 0);
+      pw = __builtin_amdgcn_raw_buffer_load_b8(rsw, st, 0, 0);
+    } else {
+      px = __builtin_amdgcn_raw_buffer_load_b32(rsx, (int)(soff + (uint32_t)st * 4u), 0, 0);
+      pw = __builtin_amdgcn_raw_buffer_load_b32(rsw, st * 4, 0, 0);
     }
   };
   auto put_scales = [&](uint32_t* ss) {
-    if (64 * w < TN) ss[64 * w + lane] = E8M0 && !HW ? __float_as_uint(e8m0_value(pend)) : pend;
+    ss[srow] = E8M0 && !HW ? __float_as_uint(e8m0_value(px)) : px;
+    ss[TN + w % WB] = E8M0 && !HW ? __float_as_uint(e8m0_value(pw)) : pw;
   };
-  uint32_t se[NB];
+  uint32_t xe[NB], we;
 
   f32x4 acc[MI][NB];
 #pragma unroll
@@ -206,7 +209,8 @@ __global__ __launch_bounds__(512, 2) void k_fp8_tile(LinearFp8Args a, int MT, in
   const uint32_t abase = (uint32_t)(16 * MI * wm + r16) * 128u + fslot, bbase = (uint32_t)(16 * NB * wn + r16) * 128u + fslot;
   auto read = [&](const uint8_t* sw, const uint8_t* sx, const uint32_t* ss) {
 #pragma unroll
-    for (int b = 0; b < NB; ++b) se[b] = ss[16 * NB * wn + 16 * b + r16];
+    for (int b = 0; b < NB; ++b) xe[b] = ss[16 * NB * wn + 16 * b + r16];
+    we = ss[TN + 16 * MI * wm / kFp8Block];
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
       fb[b][0] = *reinterpret_cast<const u32x4*>(sx + bbase + b * 2048);
@@ -218,15 +222,11 @@ __global__ __launch_bounds__(512, 2) void k_fp8_tile(LinearFp8Args a, int MT, in
       fa[i][1] = *reinterpret_cast<const u32x4*>(sw + (abase ^ 64u) + i * 2048);
     }
   };
-  auto multiply = [&](int st) {
+  auto multiply = [&]() {
     float sc[NB];
-    uint32_t swe = 0;
-    if constexpr (HW) {
-      swe = wsp[st];
-    } else {
-      const float swv = E8M0 ? e8m0_value(wsp[st]) : reinterpret_cast<const float*>(wsp)[st];
+    if constexpr (!HW) {
 #pragma unroll
-      for (int b = 0; b < NB; ++b) sc[b] = __uint_as_float(se[b]) * swv;
+      for (int b = 0; b < NB; ++b) sc[b] = __uint_as_float(xe[b]) * __uint_as_float(we);
     }
     if constexpr (PREC) {
       fp_bf16x8 xb[NB][4];
@@ -277,7 +277,7 @@ __global__ __launch_bounds__(512, 2) void k_fp8_tile(LinearFp8Args a, int MT, in
         for (int b = 0; b < NB; ++b) {
           const i32x8 wv = join8(fa[i][0], fa[i][1]), xv = join8(fb[b][0], fb[b][1]);
           if constexpr (HW) {
-            acc[i][b] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wv, xv, acc[i][b], 0, 0, 0, (int)swe, 0, (int)se[b]);
+            acc[i][b] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wv, xv, acc[i][b], 0, 0, 0, (int)we, 0, (int)xe[b]);
           } else {
             const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
             const f32x4 p = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wv, xv, zero, 0, 0, 0, 0, 0, 0);
@@ -287,6 +287,7 @@ __global__ __launch_bounds__(512, 2) void k_fp8_tile(LinearFp8Args a, int MT, in
         }
       if constexpr (!HW) {
         // a few products ahead of the sums that use them
+        __builtin_amdgcn_sched_group_barrier(0x002, NB, 0);
         __builtin_amdgcn_sched_group_barrier(0x008, 3, 0);
 #pragma unroll
         for (int i = 0; i < MI * NB - 3; ++i) {
@@ -313,7 +314,7 @@ __global__ __launch_bounds__(512, 2) void k_fp8_tile(LinearFp8Args a, int MT, in
     read(sw, sx, ss);
     wait_lds();
     phase_end();
-    multiply(st);
+    multiply();
     __builtin_amdgcn_sched_barrier(0);
     wait_vm<0>();
     put_scales(ns);
@@ -329,7 +330,7 @@ __global__ __launch_bounds__(512, 2) void k_fp8_tile(LinearFp8Args a, int MT, in
     phase_end();
     issue(sw, sx, st + 2);
     __builtin_amdgcn_sched_barrier(0);
-    multiply(st);
+    multiply();
     phase_end();
   };
   issue(sw0, sx0, 0);
