@@ -120,13 +120,57 @@ __global__ __launch_bounds__(kFewWaves * kWaveSize) void k_fp8_few(LinearFp8Args
   }
 }
 
-// Many rows: a block of eight waves owns TM outputs x TN rows of x.
+// The scales of four consecutive steps of a row, in registers.  Where fewer than
+// four are left, the row's last four; a row of fewer takes load_few.
+inline __device__ int scale_start(int st, int KB) { return max(0, min(st, KB - 4)); }
+struct __attribute__((packed, aligned(1))) u32u { uint32_t v; };
+template <bool E8M0> struct Fp8ScaleRun;
+template <> struct Fp8ScaleRun<false> {
+  f32x4u v;
+  __device__ __forceinline__ void load(const uint8_t* row, int st, int KB) {
+    v = *reinterpret_cast<const f32x4u*>(reinterpret_cast<const float*>(row) + scale_start(st, KB));
+  }
+  __device__ __forceinline__ void load_few(const uint8_t* row, int KB) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v.v[j] = j < KB ? reinterpret_cast<const float*>(row)[j] : 0.f;
+  }
+  template <bool HW> __device__ __forceinline__ uint32_t get(int j) const { return __float_as_uint(v.v[j]); }
+};
+template <> struct Fp8ScaleRun<true> {
+  uint32_t v;
+  __device__ __forceinline__ void load(const uint8_t* row, int st, int KB) {
+    v = reinterpret_cast<const u32u*>(row + scale_start(st, KB))->v;
+  }
+  __device__ __forceinline__ void load_few(const uint8_t* row, int KB) {
+    v = 0u;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v |= j < KB ? (uint32_t)row[j] << (8 * j) : 0u;
+  }
+  // the byte for the matrix instruction, or the number
+  template <bool HW> __device__ __forceinline__ uint32_t get(int j) const {
+    const uint32_t e = (v >> (8 * j)) & 255u;
+    return HW ? e : __float_as_uint(e8m0_value(e));
+  }
+};
+
+constexpr int kTileGroup = 6;
+
+// Many rows: a block of eight waves owns TM = 256 outputs x TN rows of x.
 //
 // The waves form two groups, one wave of each on every SIMD, that alternate: while
-// one multiplies the operands it holds in registers, the other reads its next
-// ones from LDS (a barrier ends each such phase), so the matrix cores never wait
-// for a read of the wave they work for.  Memory goes straight to LDS
-// two phases ahead: step s + 2 overwrites step s once both groups have read it.
+// one multiplies the operands it holds in registers (step s in phase 2 s, the
+// second group's in phase 2 s + 1), the other reads its next ones from LDS; a
+// barrier ends each phase.  Memory goes straight to LDS, two buffers of a step
+// each, and its loads are sent between products: sent all at once they hold up
+// the wave that sends them for as long as the 64 KB of a step take.  The first
+// group's outputs are the lower half of the weights (W0), the second's the upper
+// (W1), x is everyone's:
+//   phase 2 s      first group multiplies s, sends W1 of s + 1 and W0 of s + 2;
+//                  second reads W1 and x of s
+//   phase 2 s + 1  second group multiplies s, sends x of s + 2; first reads W0
+//                  and x of s + 1
+// so each part is overwritten once its readers are through with it, and has one
+// to three phases to arrive.
 template <bool PREC> struct TileGeom;
 template <> struct TileGeom<false> {
   static constexpr int WM = 2, WN = 4, MI = 8, NB = 4;  // waves, and 16 x 16 tiles of a wave
@@ -140,21 +184,28 @@ __global__ __launch_bounds__(512, 2) void k_fp8_tile(LinearFp8Args a, int MT, in
   typedef TileGeom<PREC> G;
   constexpr int MI = G::MI, NB = G::NB;
   constexpr int TM = 16 * MI * G::WM, TN = 16 * NB * G::WN;
-  constexpr int WQ = TM / 64, XQ = TN / 64;  // loads of a wave and step: 1 KB (8 rows) each
-  constexpr int WB = TM / kFp8Block;         // the weight's scales of a step
-  constexpr bool HW = E8M0 && !PREC;         // scales applied by the matrix instruction
-  __shared__ __attribute__((aligned(1024))) uint8_t sw0[TM * 128], sx0[TN * 128], sw1[TM * 128], sx1[TN * 128];
-  __shared__ uint32_t ss0[TN + WB], ss1[TN + WB];
+  static_assert(TM == 256 && MI * G::WM / 2 == 8, "a group's outputs are 128");
+  constexpr int WQ = 4, XQ = TN / 32;  // 1 KB loads (8 rows) of a wave: of a half of the weights, of x
+  constexpr bool HW = E8M0 && !PREC;   // scales applied by the matrix instruction
+  // one array per part in flight: the compiler then sees that a load into one
+  // does not touch what is read from another
+  __shared__ __attribute__((aligned(1024))) uint8_t wlo0[128 * 128], wlo1[128 * 128], whi0[128 * 128], whi1[128 * 128];
+  __shared__ __attribute__((aligned(1024))) uint8_t xb0[TN * 128], xb1[TN * 128];
+  // scales of eight steps: of the tile's rows, and of the weights' two blocks
+  __shared__ uint32_t ring[8][TN + 2];
   const int tid = threadIdx.x, lane = tid & (kWaveSize - 1);
   const int w = __builtin_amdgcn_readfirstlane(tid / kWaveSize);
-  const int wm = w / G::WN, wn = w % G::WN;
+  const int wm = w / G::WN, wn = w % G::WN, grp = w / 4, gw = w % 4;
   const int r16 = lane & 15, g = lane >> 4;
 
-  // Each XCD takes a consecutive run of tiles, rows of x fastest.
+  // Each XCD takes a consecutive run of tiles, in columns of kTileGroup tiles of
+  // outputs, so that the 32 tiles an XCD works on share operands both ways.
   const int total = MT * NT;
   const int xcd = blockIdx.x % 8, ix = blockIdx.x / 8, per = total / 8, rem = total % 8;
   const int tile = xcd * per + (xcd < rem ? xcd : rem) + ix;
-  const int mt = tile / NT, c0 = mt * TM, t0 = (tile - mt * NT) * TN;
+  const int first = tile / (kTileGroup * NT) * kTileGroup, in = tile - first * NT;
+  const int high = min(kTileGroup, MT - first);
+  const int c0 = (first + in % high) * TM, t0 = in / high * TN;
   const int KB = a.ld / kFp8Block;
   const int nc = min(TM, a.n - c0), nt = min(TN, a.N - t0);
   const __amdgpu_buffer_rsrc_t rw = make_rsrc(a.wq + (size_t)c0 * a.ld, (uint32_t)nc * a.ld);
@@ -162,40 +213,49 @@ __global__ __launch_bounds__(512, 2) void k_fp8_tile(LinearFp8Args a, int MT, in
 
   // Piece c (16 bytes) of row r lies at slot c ^ (r & 7) of its 128 bytes, so
   // that eight lanes that read the same piece of eight rows hit distinct banks.
+  // Rows past the tile's last lie past the buffer and read as zero, and so do
+  // steps past the last.
   const uint32_t loff = (uint32_t)((lane & 7) ^ (lane >> 3)) * 16u;
-  // Rows past the tile's last lie past the buffer and read as zero.
-  const uint32_t woff = (uint32_t)(8 * WQ * w + (lane >> 3)) * a.ld + loff;
-  const uint32_t xoff = (uint32_t)(8 * XQ * w + (lane >> 3)) * a.ld + loff;
-  auto issue = [&](uint8_t* sw, uint8_t* sx, int st) {
-    const uint32_t k = st < KB ? (uint32_t)st * kFp8Block : kOOB;
-#pragma unroll
-    for (int q = 0; q < WQ; ++q) dma16(rw, sw + (WQ * w + q) * 1024, woff + (k + 8u * q * a.ld));
-#pragma unroll
-    for (int q = 0; q < XQ; ++q) dma16(rx, sx + (XQ * w + q) * 1024, xoff + (k + 8u * q * a.ld));
+  const uint32_t woff = (uint32_t)(8 * WQ * gw + (lane >> 3)) * a.ld + loff;
+  const uint32_t xoff = (uint32_t)(8 * XQ * gw + (lane >> 3)) * a.ld + loff;
+  auto at = [&](int st) { return st < KB ? (uint32_t)st * kFp8Block : kOOB; };
+  // (addresses made anew for each load: kept, they cost the registers of a tile)
+  auto fresh = [](uint32_t v) {
+    asm volatile("" : "+v"(v));
+    return v;
   };
-  // The scales of a step: each wave of the first group fetches those of 64 of the
-  // tile's rows and one of the weight's into registers and, a phase later, puts them
-  // into LDS (some waves the same).  Not a load where they are used: its wait
-  // would be one for the step's operands too.
+  auto send_w = [&](uint8_t* dst, int half, int st) {
+#pragma unroll
+    for (int q = 0; q < WQ; ++q)
+      dma16(rw, dst + (WQ * gw + q) * 1024, fresh(woff) + (at(st) + (128u * half + 8u * q) * a.ld));
+  };
+  auto send_x = [&](uint8_t* dst, int st) {
+#pragma unroll
+    for (int q = 0; q < XQ; ++q) dma16(rx, dst + (XQ * gw + q) * 1024, fresh(xoff) + (at(st) + 8u * q * a.ld));
+  };
+
+  // Scales: each wave of the first group fetches those of 64 of the tile's rows and
+  // of the two weight blocks, four steps at a time (some lanes the same), and puts them into LDS a step later.  Not a load where they are used: its wait
+  // would be one for the operands under way too.  Where fewer than four steps are
+  // left, the last four of the row; where there are fewer, zeros past its end.
   constexpr uint32_t SB = E8M0 ? 1 : 4;
-  const int wb = min(c0 / kFp8Block + w % WB, (a.n - 1) / kFp8Block), srow = (64 * w + lane) % TN;
-  const __amdgpu_buffer_rsrc_t rsw = make_rsrc(static_cast<const uint8_t*>(a.ws) + (size_t)wb * KB * SB, (uint32_t)KB * SB);
-  const __amdgpu_buffer_rsrc_t rsx =
-      make_rsrc(static_cast<const uint8_t*>(a.xs) + (size_t)t0 * KB * SB, (uint32_t)nt * KB * SB);
-  const uint32_t soff = (uint32_t)srow * KB * SB;
-  uint32_t px = 0, pw = 0;
+  typedef Fp8ScaleRun<E8M0> Run;
+  const int wb = min(c0 / kFp8Block + (lane >> 5), (a.n - 1) / kFp8Block), srow = (64 * gw + lane) % TN;
+  const uint8_t* swp = static_cast<const uint8_t*>(a.ws) + (size_t)wb * KB * SB;
+  const uint8_t* sxp = static_cast<const uint8_t*>(a.xs) + (size_t)min(t0 + srow, a.N - 1) * KB * SB;
+  Run px, pw;
   auto fetch_scales = [&](int st) {
-    if constexpr (E8M0) {
-      px = __builtin_amdgcn_raw_buffer_load_b8(rsx, (int)(soff + (uint32_t)st), 0, 0);
-      pw = __builtin_amdgcn_raw_buffer_load_b8(rsw, st, 0, 0);
-    } else {
-      px = __builtin_amdgcn_raw_buffer_load_b32(rsx, (int)(soff + (uint32_t)st * 4u), 0, 0);
-      pw = __builtin_amdgcn_raw_buffer_load_b32(rsw, st * 4, 0, 0);
-    }
+    px.load(sxp, st, KB);
+    pw.load(swp, st, KB);
   };
-  auto put_scales = [&](uint32_t* ss) {
-    ss[srow] = E8M0 && !HW ? __float_as_uint(e8m0_value(px)) : px;
-    ss[TN + w % WB] = E8M0 && !HW ? __float_as_uint(e8m0_value(pw)) : pw;
+  auto put_scales = [&](int st) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int slot = (scale_start(st, KB) + j) & 7;
+      const uint32_t srow = fresh((uint32_t)(64 * gw + lane) % TN);
+      ring[slot][srow] = px.template get<HW>(j);
+      ring[slot][TN + (lane >> 5)] = pw.template get<HW>(j);
+    }
   };
   uint32_t xe[NB], we;
 
@@ -206,73 +266,84 @@ __global__ __launch_bounds__(512, 2) void k_fp8_tile(LinearFp8Args a, int MT, in
     for (int b = 0; b < NB; ++b) acc[i][b] = f32x4{0.f, 0.f, 0.f, 0.f};
   u32x4 fa[MI][2], fb[NB][2];
   const uint32_t fslot = (uint32_t)(g ^ (r16 & 7)) * 16u;
-  const uint32_t abase = (uint32_t)(16 * MI * wm + r16) * 128u + fslot, bbase = (uint32_t)(16 * NB * wn + r16) * 128u + fslot;
-  auto read = [&](const uint8_t* sw, const uint8_t* sx, const uint32_t* ss) {
+  const uint32_t abase = (uint32_t)(16 * MI * (wm % (G::WM / 2)) + r16) * 128u + fslot, bbase = (uint32_t)(16 * NB * wn + r16) * 128u + fslot;
+  auto read = [&](const uint8_t* sw, const uint8_t* sx, int st) {
+    const uint32_t* ss = ring[st & 7];
+    const uint32_t rb = fresh((uint32_t)(16 * NB * wn + r16));
 #pragma unroll
-    for (int b = 0; b < NB; ++b) xe[b] = ss[16 * NB * wn + 16 * b + r16];
-    we = ss[TN + 16 * MI * wm / kFp8Block];
+    for (int b = 0; b < NB; ++b) xe[b] = ss[rb + 16 * b];
+    we = ss[TN + grp];
+    const uint8_t *pb = sx + fresh(bbase), *pbx = sx + fresh(bbase ^ 64u);
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
-      fb[b][0] = *reinterpret_cast<const u32x4*>(sx + bbase + b * 2048);
-      fb[b][1] = *reinterpret_cast<const u32x4*>(sx + (bbase ^ 64u) + b * 2048);
+      fb[b][0] = *reinterpret_cast<const u32x4*>(pb + b * 2048);
+      fb[b][1] = *reinterpret_cast<const u32x4*>(pbx + b * 2048);
     }
+    const uint8_t *pa = sw + fresh(abase), *pax = sw + fresh(abase ^ 64u);
 #pragma unroll
     for (int i = 0; i < MI; ++i) {
-      fa[i][0] = *reinterpret_cast<const u32x4*>(sw + abase + i * 2048);
-      fa[i][1] = *reinterpret_cast<const u32x4*>(sw + (abase ^ 64u) + i * 2048);
+      fa[i][0] = *reinterpret_cast<const u32x4*>(pa + i * 2048);
+      fa[i][1] = *reinterpret_cast<const u32x4*>(pax + i * 2048);
     }
   };
-  auto multiply = [&]() {
-    float sc[NB];
-    if constexpr (!HW) {
+  // The products of outputs I0 .. I1 - 1 of the wave's MI, and between them SENDS
+  // loads, sent by `send` before.
+  float sc[NB];
+  fp_bf16x8 xw[PREC ? NB : 1][4];
+  auto multiply = [&](auto i0, auto i1, auto sends) {
+    constexpr int I0 = decltype(i0)::v, I1 = decltype(i1)::v, SENDS = decltype(sends)::v;
+    constexpr int TILES = (I1 - I0) * NB;
+    if constexpr (I0 == 0 && !HW) {
 #pragma unroll
       for (int b = 0; b < NB; ++b) sc[b] = __uint_as_float(xe[b]) * __uint_as_float(we);
     }
     if constexpr (PREC) {
-      fp_bf16x8 xb[NB][4];
+      if constexpr (I0 == 0) {
 #pragma unroll
-      for (int b = 0; b < NB; ++b)
+        for (int b = 0; b < NB; ++b)
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          xb[b][2 * h] = widen8(fb[b][h].x, fb[b][h].y, 1.f);
-          xb[b][2 * h + 1] = widen8(fb[b][h].z, fb[b][h].w, 1.f);
-        }
+          for (int h = 0; h < 2; ++h) {
+            xw[b][2 * h] = widen8(fb[b][h].x, fb[b][h].y, 1.f);
+            xw[b][2 * h + 1] = widen8(fb[b][h].z, fb[b][h].w, 1.f);
+          }
+      }
 #pragma unroll
-      for (int i = 0; i < MI; ++i) {
+      for (int i = I0; i < I1; ++i) {
         f32x4 p[NB];
 #pragma unroll
         for (int b = 0; b < NB; ++b) p[b] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
           const u32x4 v = fa[i][k >> 1];
-          const fp_bf16x8 wb = (k & 1) ? widen8(v.z, v.w, 1.f) : widen8(v.x, v.y, 1.f);
+          const fp_bf16x8 wv = (k & 1) ? widen8(v.z, v.w, 1.f) : widen8(v.x, v.y, 1.f);
 #pragma unroll
-          for (int b = 0; b < NB; ++b) p[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wb, xb[b][k], p[b], 0, 0, 0);
+          for (int b = 0; b < NB; ++b) p[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv, xw[b][k], p[b], 0, 0, 0);
         }
 #pragma unroll
         for (int b = 0; b < NB; ++b)
 #pragma unroll
           for (int e = 0; e < 4; ++e) acc[i][b][e] = fmaf(p[b][e], sc[b], acc[i][b][e]);
       }
-      // the first outputs' products among x's conversions, then each outputs'
-      // conversions and the sums of those before among the products
+      // x's conversions among the first products, then each outputs'
+      // conversions and the sums of those before
+      if constexpr (I0 == 0) {
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        __builtin_amdgcn_sched_group_barrier(0x002, 4 + 4 * NB, 0);
-        __builtin_amdgcn_sched_group_barrier(0x008, NB, 0);
-      }
-#pragma unroll
-      for (int k = 0; k < 4 * MI - 4; ++k) {
-#pragma unroll
-        for (int b = 0; b < NB; ++b) {
-          __builtin_amdgcn_sched_group_barrier(0x002, 1 + 4 / NB, 0);
-          __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        for (int k = 0; k < 4; ++k) {
+          __builtin_amdgcn_sched_group_barrier(0x002, 4 + 4 * NB, 0);
+          __builtin_amdgcn_sched_group_barrier(0x008, NB, 0);
         }
+      }
+      constexpr int REST = 4 * TILES - (I0 == 0 ? 4 * NB : 0);
+#pragma unroll
+      for (int k = 0; k < REST; ++k) {
+        __builtin_amdgcn_sched_group_barrier(0x002, 2, 0);
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        if (SENDS > 0 && k % (REST / SENDS) == 0) __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
       }
       __builtin_amdgcn_sched_group_barrier(0x002, 4 * NB, 0);
     } else {
 #pragma unroll
-      for (int i = 0; i < MI; ++i)
+      for (int i = I0; i < I1; ++i)
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
           const i32x8 wv = join8(fa[i][0], fa[i][1]), xv = join8(fb[b][0], fb[b][1]);
@@ -285,18 +356,26 @@ __global__ __launch_bounds__(512, 2) void k_fp8_tile(LinearFp8Args a, int MT, in
             for (int e = 0; e < 4; ++e) acc[i][b][e] = fmaf(p[e], sc[b], acc[i][b][e]);
           }
         }
-      if constexpr (!HW) {
+      if constexpr (HW) {
+#pragma unroll
+        for (int k = 0; k < TILES; ++k) {
+          __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+          if (SENDS > 0 && k % (TILES / SENDS) == 0) __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
+        }
+      } else {
         // a few products ahead of the sums that use them
-        __builtin_amdgcn_sched_group_barrier(0x002, NB, 0);
+        if (I0 == 0) __builtin_amdgcn_sched_group_barrier(0x002, NB, 0);
         __builtin_amdgcn_sched_group_barrier(0x008, 3, 0);
 #pragma unroll
-        for (int i = 0; i < MI * NB - 3; ++i) {
+        for (int k = 0; k < TILES - 3; ++k) {
           __builtin_amdgcn_sched_group_barrier(0x002, 4, 0);
           __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+          if (SENDS > 0 && k % (TILES / SENDS) == 0) __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
         }
         __builtin_amdgcn_sched_group_barrier(0x002, 12, 0);
       }
     }
+    __builtin_amdgcn_sched_barrier(0);
   };
   auto phase_end = [&]() {
     __builtin_amdgcn_sched_barrier(0);
@@ -305,58 +384,79 @@ __global__ __launch_bounds__(512, 2) void k_fp8_tile(LinearFp8Args a, int MT, in
     __builtin_amdgcn_sched_barrier(0);
   };
 
-  // A step of the first group: it sends step s + 1's loads as it reads step s (its
-  // multiply phase of the step before and the second group's read phase of
-  // that step are over), and waits for them in its multiply phase.
-  auto first_step = [&](uint8_t* sw, uint8_t* sx, uint32_t* ss, uint8_t* nw, uint8_t* nx, uint32_t* ns, int st) {
-    issue(nw, nx, st + 1);
-    fetch_scales(st + 1);
-    read(sw, sx, ss);
+  constexpr Const<0> none;
+  constexpr Const<MI / 2> half;
+  constexpr Const<MI> all;
+  // A step of the first group, FETCH: with the loads of the scales of steps st + 4
+  // on, which step st + 1 (PUT) puts into the ring.  Loads complete in order: with
+  // st's W1 there, st + 1's W0 (and the two of scales) may be under way; with that
+  // there too, the parts sent in this step.
+  auto first_step = [&](uint8_t* wlo, uint8_t* next_whi, const uint8_t* xb, int st, auto fetch, auto put) {
+    constexpr int F = decltype(fetch)::v ? 2 : 0;
+    if constexpr (decltype(fetch)::v) fetch_scales(st + 4);
+    read(wlo, xb, st);
+    wait_vm<WQ + F>();
+    if constexpr (decltype(put)::v) put_scales(st + 3);
     wait_lds();
     phase_end();
-    multiply();
-    __builtin_amdgcn_sched_barrier(0);
-    wait_vm<0>();
-    put_scales(ns);
-    wait_lds();
+    send_w(next_whi, 1, st + 1);
+    multiply(none, half, Const<WQ>());
+    send_w(wlo, 0, st + 2);
+    multiply(half, all, Const<WQ>());
+    wait_vm<2 * WQ + F>();
     phase_end();
   };
-  // The second group, a phase behind: step s + 2's loads as it multiplies step s,
-  // waited for after it has read step s + 1.
-  auto second_step = [&](uint8_t* sw, uint8_t* sx, uint32_t* ss, int st) {
-    read(sw, sx, ss);
+  auto second_step = [&](const uint8_t* whi, uint8_t* xb, int st) {
+    read(whi, xb, st);
     wait_lds();
     wait_vm<0>();
     phase_end();
-    issue(sw, sx, st + 2);
-    __builtin_amdgcn_sched_barrier(0);
-    multiply();
+    send_x(xb, st + 2);
+    multiply(none, half, Const<XQ>());
+    multiply(half, all, none);
     phase_end();
   };
-  issue(sw0, sx0, 0);
+  constexpr Const<1> yes;
   int st = 0;
-  if (w < 4) {
-    fetch_scales(0);
-    wait_vm<0>();
-    put_scales(ss0);
+  if (grp == 0) {
+    if (KB >= 4) {
+      fetch_scales(0);
+    } else {
+      px.load_few(sxp, KB);
+      pw.load_few(swp, KB);
+    }
+    send_w(wlo0, 0, 0);
+    send_w(whi0, 1, 0);
+    __builtin_amdgcn_sched_barrier(0);
+    send_w(wlo1, 0, 1);
+    __builtin_amdgcn_sched_barrier(0);
+    wait_vm<WQ>();
+    put_scales(0);
     wait_lds();
     phase_end();
-    for (; st + 2 <= KB; st += 2) {
-      first_step(sw0, sx0, ss0, sw1, sx1, ss1, st);
-      first_step(sw1, sx1, ss1, sw0, sx0, ss0, st + 1);
+    for (; st + 4 <= KB; st += 4) {
+      first_step(wlo0, whi1, xb0, st, yes, none);
+      first_step(wlo1, whi0, xb1, st + 1, none, yes);
+      first_step(wlo0, whi1, xb0, st + 2, none, none);
+      first_step(wlo1, whi0, xb1, st + 3, none, none);
     }
-    if (st < KB) first_step(sw0, sx0, ss0, sw1, sx1, ss1, st);
+    if (st < KB) first_step(wlo0, whi1, xb0, st, none, none);
+    if (st + 1 < KB) first_step(wlo1, whi0, xb1, st + 1, none, none);
+    if (st + 2 < KB) first_step(wlo0, whi1, xb0, st + 2, none, none);
     phase_end();
   } else {
-    issue(sw1, sx1, 1);
-    wait_vm<WQ + XQ>();
+    send_x(xb0, 0);
+    __builtin_amdgcn_sched_barrier(0);
+    send_x(xb1, 1);
+    __builtin_amdgcn_sched_barrier(0);
+    wait_vm<XQ>();
     phase_end();
     phase_end();
     for (; st + 2 <= KB; st += 2) {
-      second_step(sw0, sx0, ss0, st);
-      second_step(sw1, sx1, ss1, st + 1);
+      second_step(whi0, xb0, st);
+      second_step(whi1, xb1, st + 1);
     }
-    if (st < KB) second_step(sw0, sx0, ss0, st);
+    if (st < KB) second_step(whi0, xb0, st);
   }
   wait_vm<0>();  // no load is on its way to LDS when the block ends
 
