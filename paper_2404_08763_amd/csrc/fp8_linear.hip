@@ -22,6 +22,15 @@ __device__ __forceinline__ fp_bf16x8 widen8(uint32_t lo, uint32_t hi, float scal
   return fp_bf16x8{a.x, a.y, b.x, b.y, c.x, c.y, d.x, d.y};
 }
 
+// A lane's 32 values of a column block.
+__device__ __forceinline__ void widen32(const u32x4 (&v)[2], fp_bf16x8 (&f)[4]) {
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    f[2 * h] = widen8(v[h].x, v[h].y, 1.f);
+    f[2 * h + 1] = widen8(v[h].z, v[h].w, 1.f);
+  }
+}
+
 // A scale as fp32.
 __device__ __forceinline__ float e8m0_value(uint32_t e) {
   return e == 255u ? __uint_as_float(0x7fc00000u) : e == 0u ? 0x1p-127f : __uint_as_float(e << 23);
@@ -258,6 +267,7 @@ __global__ __launch_bounds__(512, 2) void k_fp8_tile(LinearFp8Args a, int MT, in
     }
   };
   uint32_t xe[NB], we;
+  fp_bf16x8 xw[PREC ? NB : 1][4], ww[PREC ? MI : 1][4];
 
   f32x4 acc[MI][NB];
 #pragma unroll
@@ -285,11 +295,16 @@ __global__ __launch_bounds__(512, 2) void k_fp8_tile(LinearFp8Args a, int MT, in
       fa[i][0] = *reinterpret_cast<const u32x4*>(pa + i * 2048);
       fa[i][1] = *reinterpret_cast<const u32x4*>(pax + i * 2048);
     }
+    if constexpr (PREC) {
+#pragma unroll
+      for (int b = 0; b < NB; ++b) widen32(fb[b], xw[b]);
+#pragma unroll
+      for (int i = 0; i < MI; ++i) widen32(fa[i], ww[i]);
+    }
   };
   // The products of outputs I0 .. I1 - 1 of the wave's MI, and between them SENDS
   // loads, sent by `send` before.
   float sc[NB];
-  fp_bf16x8 xw[PREC ? NB : 1][4];
   auto multiply = [&](auto i0, auto i1, auto sends) {
     constexpr int I0 = decltype(i0)::v, I1 = decltype(i1)::v, SENDS = decltype(sends)::v;
     constexpr int TILES = (I1 - I0) * NB;
@@ -298,15 +313,6 @@ __global__ __launch_bounds__(512, 2) void k_fp8_tile(LinearFp8Args a, int MT, in
       for (int b = 0; b < NB; ++b) sc[b] = __uint_as_float(xe[b]) * __uint_as_float(we);
     }
     if constexpr (PREC) {
-      if constexpr (I0 == 0) {
-#pragma unroll
-        for (int b = 0; b < NB; ++b)
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            xw[b][2 * h] = widen8(fb[b][h].x, fb[b][h].y, 1.f);
-            xw[b][2 * h + 1] = widen8(fb[b][h].z, fb[b][h].w, 1.f);
-          }
-      }
 #pragma unroll
       for (int i = I0; i < I1; ++i) {
         f32x4 p[NB];
@@ -314,31 +320,21 @@ __global__ __launch_bounds__(512, 2) void k_fp8_tile(LinearFp8Args a, int MT, in
         for (int b = 0; b < NB; ++b) p[b] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-          const u32x4 v = fa[i][k >> 1];
-          const fp_bf16x8 wv = (k & 1) ? widen8(v.z, v.w, 1.f) : widen8(v.x, v.y, 1.f);
 #pragma unroll
-          for (int b = 0; b < NB; ++b) p[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv, xw[b][k], p[b], 0, 0, 0);
+          for (int b = 0; b < NB; ++b) p[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ww[i][k], xw[b][k], p[b], 0, 0, 0);
         }
 #pragma unroll
         for (int b = 0; b < NB; ++b)
 #pragma unroll
           for (int e = 0; e < 4; ++e) acc[i][b][e] = fmaf(p[b][e], sc[b], acc[i][b][e]);
       }
-      // x's conversions among the first products, then each outputs'
-      // conversions and the sums of those before
-      if constexpr (I0 == 0) {
+      // the sums of one row of tiles among the products of the next
+      if (I0 == 0) __builtin_amdgcn_sched_group_barrier(0x002, NB, 0);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          __builtin_amdgcn_sched_group_barrier(0x002, 4 + 4 * NB, 0);
-          __builtin_amdgcn_sched_group_barrier(0x008, NB, 0);
-        }
-      }
-      constexpr int REST = 4 * TILES - (I0 == 0 ? 4 * NB : 0);
-#pragma unroll
-      for (int k = 0; k < REST; ++k) {
-        __builtin_amdgcn_sched_group_barrier(0x002, 2, 0);
+      for (int k = 0; k < 4 * TILES; ++k) {
         __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-        if (SENDS > 0 && k % (REST / SENDS) == 0) __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
+        if (k >= 4 * NB) __builtin_amdgcn_sched_group_barrier(0x002, 1, 0);
+        if (SENDS > 0 && k % (4 * TILES / SENDS) == 0) __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
       }
       __builtin_amdgcn_sched_group_barrier(0x002, 4 * NB, 0);
     } else {
