@@ -137,7 +137,8 @@ cats_status cats_silu_mul_fp8(const void* gate_up, int32_t dtype, int32_t N, int
 
 size_t cats_linear_fp8_workspace_bytes(int32_t N, int32_t n, int32_t k) {
   if (!linear_shape_ok(N, n, k)) return 0;
-  return kWsAlign;
+  const size_t bytes = cats::linear_fp8_partial_bytes(N, n, (int)blocks_of(k));
+  return bytes < kWsAlign ? kWsAlign : (bytes + kWsAlign - 1) / kWsAlign * kWsAlign;
 }
 
 cats_status cats_linear_fp8(const void* xq, const void* xs, int32_t N, const void* wq, const void* wscale, int32_t n,
@@ -177,6 +178,7 @@ cats_status cats_linear_fp8(const void* xq, const void* xs, int32_t N, const voi
   a.ld = (int)ld;
   a.e8m0 = stype == CATS_SCALE_E8M0;
   a.ybf16 = ydtype == CATS_BF16;
+  a.partial = static_cast<float*>(ws);
   return launched(cats::launch_linear_fp8(a, static_cast<hipStream_t>(stream)), stream, "cats_linear_fp8");
 }
 

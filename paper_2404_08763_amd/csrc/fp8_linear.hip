@@ -8,10 +8,9 @@
 namespace cats {
 
 typedef int i32x8 __attribute__((ext_vector_type(8)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef __bf16 fp_bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 fp_bf16x2 __attribute__((ext_vector_type(2)));
-
-constexpr int kFewWaves = 8;  // waves of a block, each taking every eighth column block
 
 // Eight e4m3 values times 2^e (scale = 2^e) as bf16, which holds them exactly.
 __device__ __forceinline__ fp_bf16x8 widen8(uint32_t lo, uint32_t hi, float scale) {
@@ -20,6 +19,39 @@ __device__ __forceinline__ fp_bf16x8 widen8(uint32_t lo, uint32_t hi, float scal
   const fp_bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false);
   const fp_bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true);
   return fp_bf16x8{a.x, a.y, b.x, b.y, c.x, c.y, d.x, d.y};
+}
+
+// A scale as fp32.
+__device__ __forceinline__ float e8m0_value(uint32_t e) {
+  // (0 is 2^-127, a subnormal, and 255 NaN: both have the uppermost mantissa bit)
+  return __uint_as_float((e << 23) | (e - 1u < 254u ? 0u : 0x400000u));
+}
+
+// A scale as it is stored, from a buffer, and as a number.
+template <bool E8M0> __device__ __forceinline__ uint32_t scale_load(const __amdgpu_buffer_rsrc_t& r, uint32_t at) {
+  if constexpr (E8M0) return __builtin_amdgcn_raw_buffer_load_b8(r, (int)at, 0, 0);
+  else return __builtin_amdgcn_raw_buffer_load_b32(r, (int)at, 0, 0);
+}
+template <bool E8M0> __device__ __forceinline__ float scale_value(uint32_t s) {
+  return E8M0 ? e8m0_value(s) : __uint_as_float(s);
+}
+
+// From two loads of eight rows' whole lines (lane r + 16 g: piece g, or g + 4 for
+// r >= 8, of row r % 8, and of row r % 8 + 8) pieces g and g + 4 of row r.
+__device__ __forceinline__ void whole_rows(const u32x4 (&l)[2], u32x4 (&v)[2]) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {  // row_ror:8, into lanes 8 .. 15 and 0 .. 7 of each 16
+    v[0][e] = (uint32_t)__builtin_amdgcn_update_dpp((int)l[0][e], (int)l[1][e], 0x128, 0xf, 0xc, false);
+    v[1][e] = (uint32_t)__builtin_amdgcn_update_dpp((int)l[1][e], (int)l[0][e], 0x128, 0xf, 0x3, false);
+  }
+}
+
+// A value the compiler knows nothing about: that it is the same for all lanes (it
+// would move what is loaded through it to a scalar register, and wait for it at
+// once), or what addresses made from it could be kept.
+__device__ __forceinline__ uint32_t fresh(uint32_t v) {
+  asm volatile("" : "+v"(v));
+  return v;
 }
 
 // A lane's 32 values of a column block.
@@ -31,30 +63,10 @@ __device__ __forceinline__ void widen32(const u32x4 (&v)[2], fp_bf16x8 (&f)[4]) 
   }
 }
 
-// A scale as fp32.
-__device__ __forceinline__ float e8m0_value(uint32_t e) {
-  return e == 255u ? __uint_as_float(0x7fc00000u) : e == 0u ? 0x1p-127f : __uint_as_float(e << 23);
-}
-template <bool E8M0> __device__ __forceinline__ float scale_at(const void* s, size_t i) {
-  return E8M0 ? e8m0_value(static_cast<const uint8_t*>(s)[i]) : static_cast<const float*>(s)[i];
-}
 
-// The products of one column block, 16 weights by 16 rows: weights are the first
-// operand and rows of x the second, so a lane's four results are four
-// consecutive outputs of one row.  Which of the block's columns sit in which
-// lane does not matter as long as both operands agree: lane l holds bytes
-// 16 (l / 16) .. + 15 and 64 more of row l % 16.
-// The values go through the bf16 instructions, whose sums are exact to fp32;
-// the 8-bit ones drop what lies 2^-13 below the largest of each eight products
-// (4e-5 of the result on rows with outliers, in the mean square).
-__device__ __forceinline__ f32x4 block_product(const u32x4 (&w)[2], const u32x4 (&x)[2]) {
-  f32x4 p = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    p = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen8(w[h].x, w[h].y, 1.f), widen8(x[h].x, x[h].y, 1.f), p, 0, 0, 0);
-    p = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen8(w[h].z, w[h].w, 1.f), widen8(x[h].z, x[h].w, 1.f), p, 0, 0, 0);
-  }
-  return p;
+// Values 8 k .. 8 k + 7 of a lane's 16.
+__device__ __forceinline__ fp_bf16x8 widen_part(const u32x4& v, int k) {
+  return k ? widen8(v.z, v.w, 1.f) : widen8(v.x, v.y, 1.f);
 }
 
 __device__ __forceinline__ i32x8 join8(const u32x4& a, const u32x4& b) {
@@ -90,43 +102,216 @@ __device__ __forceinline__ void put_y4(const LinearFp8Args& a, size_t i, f32x4 v
   }
 }
 
-// 16 outputs x 16 rows per block, its waves splitting the column blocks.
-template <bool E8M0>
-__global__ __launch_bounds__(kFewWaves * kWaveSize) void k_fp8_few(LinearFp8Args a) {
-  __shared__ f32x4 red[kFewWaves][kWaveSize];
+// Up to 16 rows (32 with NB = 2) whose C column blocks a wave can keep: a block a
+// compute unit goes through the tiles of 16 outputs.  Its 16 waves split the column
+// blocks (wave w takes w, w + 16, ..), keep x's in registers for all tiles and
+// always have the next tile's weights under way, also while the waves add up a
+// tile (a barrier that waits for LDS alone).  Bound by the weights' stream: a load
+// instruction reads whole 128-byte lines, of eight rows (rows r and r + 8 in two
+// loads, then lanes r and r + 8 exchange halves: 4096 -> 22016 of one row 16.6 us,
+// 22.1 with 64 bytes of 16 rows).  4096 -> 22016: 5.4 TB/s, launch included, of
+// the 7.2 that a large plain read reaches.
+constexpr int kStreamWaves = 16;
+template <int C, int NB, bool E8M0, bool RES>
+__global__ __launch_bounds__(64 * kStreamWaves) void k_fp8_stream(LinearFp8Args a, int CT) {
+  constexpr int W = kStreamWaves;
+  __shared__ f32x4 red[2][W][NB][kWaveSize];
   const int tid = threadIdx.x, lane = tid & (kWaveSize - 1);
   const int w = __builtin_amdgcn_readfirstlane(tid / kWaveSize);
   const int r16 = lane & 15, g = lane >> 4;
-  const int c0 = blockIdx.x * 16, t0 = blockIdx.y * 16;
   const int KB = a.ld / kFp8Block;
-  const int nc = min(16, a.n - c0), nt = min(16, a.N - t0);
-  const __amdgpu_buffer_rsrc_t rw = make_rsrc(a.wq + (size_t)c0 * a.ld, (uint32_t)nc * a.ld);
-  const __amdgpu_buffer_rsrc_t rx = make_rsrc(a.xq + (size_t)t0 * a.ld, (uint32_t)nt * a.ld);
-  const uint32_t woff = r16 < nc ? (uint32_t)r16 * a.ld + g * 16u : kOOB;
-  const uint32_t xoff = r16 < nt ? (uint32_t)r16 * a.ld + g * 16u : kOOB;
-  const size_t xsrow = (size_t)(t0 + (r16 < nt ? r16 : 0)) * KB, wsrow = (size_t)(c0 / kFp8Block) * KB;
-  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-  for (int b = w; b < KB; b += kFewWaves) {
-    const uint32_t k = (uint32_t)b * kFp8Block;
-    const u32x4 wv[2] = {ld_buf16_stream(rw, woff + k), ld_buf16_stream(rw, woff + k + 64u)};
-    const u32x4 xv[2] = {ld_buf16(rx, xoff + k), ld_buf16(rx, xoff + k + 64u)};
-    const f32x4 p = block_product(wv, xv);
-    const float scale = scale_at<E8M0>(a.xs, xsrow + b) * scale_at<E8M0>(a.ws, wsrow + b);
+  constexpr uint32_t SB = E8M0 ? 1 : 4;
+  // x: rows past the last, and column blocks past the last, read as zero
+  u32x4 x[C][NB][2];
+  float sx[C][NB];
+  {
+    const __amdgpu_buffer_rsrc_t rx = make_rsrc(a.xq, (uint32_t)a.N * a.ld);
+    const __amdgpu_buffer_rsrc_t rsx = make_rsrc(a.xs, (uint32_t)a.N * KB * SB);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) acc[e] = fmaf(p[e], scale, acc[e]);
+    for (int u = 0; u < C; ++u) {
+      const int b = w + W * u;
+      const uint32_t out = b < KB ? 0u : kOOB;
+#pragma unroll
+      for (int j = 0; j < NB; ++j) {
+        const uint32_t at = out + (uint32_t)(16 * j + r16) * a.ld + (uint32_t)b * kFp8Block + g * 16u;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) x[u][j][h] = ld_buf16(rx, at + 64u * h);
+        sx[u][j] = scale_value<E8M0>(scale_load<E8M0>(rsx, out + ((uint32_t)(16 * j + r16) * KB + b) * SB));
+      }
+    }
+  }
+  u32x4 wl[C][2];
+  uint32_t sw[C];
+  const uint32_t woff = (uint32_t)(r16 & 7) * a.ld + (uint32_t)(g + 4 * (r16 >> 3)) * 16u;
+  const int ot = tid >> 4, oc = tid & 15;  // the output this thread adds up (256 or 512 of them)
+  auto load = [&](int u, int ct) {
+    const int b = w + W * u, c0 = ct * 16;
+    const bool in = b < KB && ct < CT;
+    const __amdgpu_buffer_rsrc_t rw = make_rsrc(a.wq + (size_t)(in ? c0 : 0) * a.ld, (uint32_t)min(16, a.n - (in ? c0 : 0)) * a.ld);
+    const uint32_t at = woff + (in ? (uint32_t)b * kFp8Block : kOOB);
+    wl[u][0] = ld_buf16_stream(rw, at);
+    wl[u][1] = ld_buf16_stream(rw, at + 8u * a.ld);
+    const __amdgpu_buffer_rsrc_t rsw =
+        make_rsrc(static_cast<const uint8_t*>(a.ws) + (size_t)((in ? c0 : 0) / kFp8Block) * KB * SB, (uint32_t)KB * SB);
+    sw[u] = scale_load<E8M0>(rsw, fresh(in ? (uint32_t)b * SB : kOOB));
+  };
+  const uint32_t yb = a.ybf16 ? 2 : 4, ybytes = (uint32_t)a.N * a.n * yb;
+  const __amdgpu_buffer_rsrc_t ry = make_rsrc(a.y, ybytes), rr = make_rsrc(a.residual, ybytes);
+  auto y_at = [&](int ct) { return ot < a.N && ct * 16 + oc < a.n ? (uint32_t)(ot * a.n + ct * 16 + oc) * yb : kOOB; };
+  int ct = blockIdx.x;
+#pragma unroll
+  for (int u = 0; u < C; ++u) {
+    __builtin_amdgcn_sched_barrier(0);
+    load(u, ct);
+  }
+  __builtin_amdgcn_sched_barrier(0);
+  for (int turn = 0; ct < CT; ct += gridDim.x, turn ^= 1) {
+    f32x4 acc[NB];
+#pragma unroll
+    for (int j = 0; j < NB; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int u = 0; u < C; ++u) {
+      u32x4 v[2];
+      fp_bf16x8 wv[4];
+      whole_rows(wl[u], v);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) wv[k] = widen_part(v[k >> 1], k & 1);
+      float s[NB];
+#pragma unroll
+      for (int j = 0; j < NB; ++j) s[j] = sx[u][j] * scale_value<E8M0>(sw[u]);
+      // the next tile's loads go out before the products, into the registers that
+      // the exchange has just left (into others, a copy would wait for them)
+      __builtin_amdgcn_sched_barrier(0);
+      load(u, ct + gridDim.x);
+      __builtin_amdgcn_sched_barrier(0);
+      f32x4 p[NB];
+#pragma unroll
+      for (int j = 0; j < NB; ++j) p[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+#pragma unroll
+        for (int j = 0; j < NB; ++j)
+          p[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv[k], widen_part(x[u][j][k >> 1], k & 1), p[j], 0, 0, 0);
+      }
+#pragma unroll
+      for (int j = 0; j < NB; ++j) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[j][e] = fmaf(p[j][e], s[j], acc[j][e]);
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < NB; ++j) red[turn][w][j][lane] = acc[j];
+    wait_lds();
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    if (tid < NB * 256) {
+      float part[W], v = 0.f;
+#pragma unroll
+      for (int q = 0; q < W; ++q) part[q] = red[turn][q][ot >> 4][(ot & 15) + 16 * (oc >> 2)][oc & 3];
+#pragma unroll
+      for (int q = 0; q < W; ++q) v += part[q];
+      const uint32_t at = y_at(ct);
+      if constexpr (RES)
+        v += a.ybf16 ? bf16_value((uint16_t)__builtin_amdgcn_raw_buffer_load_b16(rr, (int)at, 0, 0))
+                     : __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rr, (int)at, 0, 0));
+      if (a.ybf16) __builtin_amdgcn_raw_buffer_store_b16((short)bf16_bits(v), ry, (int)at, 0, 0);
+      else __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v), ry, (int)at, 0, 0);
+    }
+  }
+}
+
+template <int C, int NB>
+static hipError_t launch_stream(const LinearFp8Args& a, hipStream_t s) {
+  const int CT = (a.n + 15) / 16, each = (CT + 255) / 256;
+  const dim3 grid((CT + each - 1) / each), block(64 * kStreamWaves);
+  KernelTimer timer("linear_fp8_stream", s);
+  if (a.e8m0 && a.residual)
+    hipExtLaunchKernelGGL((k_fp8_stream<C, NB, true, true>), grid, block, 0, s, timer.start(), timer.stop(), 0, a, CT);
+  else if (a.e8m0)
+    hipExtLaunchKernelGGL((k_fp8_stream<C, NB, true, false>), grid, block, 0, s, timer.start(), timer.stop(), 0, a, CT);
+  else if (a.residual)
+    hipExtLaunchKernelGGL((k_fp8_stream<C, NB, false, true>), grid, block, 0, s, timer.start(), timer.stop(), 0, a, CT);
+  else
+    hipExtLaunchKernelGGL((k_fp8_stream<C, NB, false, false>), grid, block, 0, s, timer.start(), timer.stop(), 0, a, CT);
+  return hipGetLastError();
+}
+
+// Up to 16 rows of more column blocks than that: a block owns 16 outputs, its
+// waves split the column blocks the same way, weights and x two column blocks
+// ahead in registers.
+template <bool E8M0>
+__global__ __launch_bounds__(64 * kStreamWaves) void k_fp8_split(LinearFp8Args a) {
+  constexpr int W = kStreamWaves, D = 2;
+  __shared__ f32x4 red[W][kWaveSize];
+  const int tid = threadIdx.x, lane = tid & (kWaveSize - 1);
+  const int w = __builtin_amdgcn_readfirstlane(tid / kWaveSize);
+  const int r16 = lane & 15, g = lane >> 4;
+  const int c0 = blockIdx.x * 16, KB = a.ld / kFp8Block;
+  const int nc = min(16, a.n - c0);
+  constexpr uint32_t SB = E8M0 ? 1 : 4;
+  const __amdgpu_buffer_rsrc_t rw = make_rsrc(a.wq + (size_t)c0 * a.ld, (uint32_t)nc * a.ld);
+  const __amdgpu_buffer_rsrc_t rx = make_rsrc(a.xq, (uint32_t)a.N * a.ld);
+  const __amdgpu_buffer_rsrc_t rsx = make_rsrc(a.xs, (uint32_t)a.N * KB * SB);
+  const __amdgpu_buffer_rsrc_t rsw =
+      make_rsrc(static_cast<const uint8_t*>(a.ws) + (size_t)(c0 / kFp8Block) * KB * SB, (uint32_t)KB * SB);
+  const uint32_t woff = (uint32_t)(r16 & 7) * a.ld + (uint32_t)(g + 4 * (r16 >> 3)) * 16u;
+  const uint32_t xoff = (uint32_t)r16 * a.ld + g * 16u, soff = (uint32_t)r16 * KB * SB;
+  u32x4 wl[D][2], x[D][2];
+  uint32_t sw[D], sx[D];
+  auto load = [&](int u, int b) {
+    const uint32_t k = b < KB ? (uint32_t)b * kFp8Block : kOOB, s = b < KB ? (uint32_t)b * SB : kOOB;
+    wl[u][0] = ld_buf16_stream(rw, woff + k);
+    wl[u][1] = ld_buf16_stream(rw, woff + k + 8u * a.ld);
+    x[u][0] = ld_buf16(rx, xoff + k);
+    x[u][1] = ld_buf16(rx, xoff + k + 64u);
+    sx[u] = scale_load<E8M0>(rsx, soff + s);
+    sw[u] = scale_load<E8M0>(rsw, fresh(s));
+  };
+  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int u = 0; u < D; ++u) {
+    __builtin_amdgcn_sched_barrier(0);
+    load(u, w + u * W);
+  }
+  __builtin_amdgcn_sched_barrier(0);
+  for (int b = w; b < KB; b += D * W) {
+#pragma unroll
+    for (int u = 0; u < D; ++u) {
+      u32x4 v[2];
+      whole_rows(wl[u], v);
+      const float s = scale_value<E8M0>(sx[u]) * scale_value<E8M0>(sw[u]);
+      f32x4 p = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        p = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen_part(v[k >> 1], k & 1), widen_part(x[u][k >> 1], k & 1), p, 0, 0, 0);
+      __builtin_amdgcn_sched_barrier(0);
+      load(u, b + (u + D) * W);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[e] = fmaf(p[e], s, acc[e]);
+    }
   }
   red[w][lane] = acc;
   __syncthreads();
   if (tid < 256) {
     const int t = tid >> 4, c = tid & 15;
-    if (t < nt && c < nc) {
-      const int l = t + 16 * (c >> 2), e = c & 3;
+    if (t < a.N && c < nc) {
       float v = 0.f;
 #pragma unroll
-      for (int i = 0; i < kFewWaves; ++i) v += red[i][l][e];
-      put_y(a, (size_t)(t0 + t) * a.n + c0 + c, v);
+      for (int q = 0; q < W; ++q) v += red[q][t + 16 * (c >> 2)][c & 3];
+      put_y(a, (size_t)t * a.n + c0 + c, v);
     }
   }
+}
+
+static hipError_t launch_split(const LinearFp8Args& a, hipStream_t s) {
+  const dim3 grid((a.n + 15) / 16), block(64 * kStreamWaves);
+  KernelTimer timer("linear_fp8_split", s);
+  if (a.e8m0)
+    hipExtLaunchKernelGGL((k_fp8_split<true>), grid, block, 0, s, timer.start(), timer.stop(), 0, a);
+  else
+    hipExtLaunchKernelGGL((k_fp8_split<false>), grid, block, 0, s, timer.start(), timer.stop(), 0, a);
+  return hipGetLastError();
 }
 
 // The scales of four consecutive steps of a row, in registers.  Where fewer than
@@ -228,11 +413,6 @@ __global__ __launch_bounds__(512, 2) void k_fp8_tile(LinearFp8Args a, int MT, in
   const uint32_t woff = (uint32_t)(8 * WQ * gw + (lane >> 3)) * a.ld + loff;
   const uint32_t xoff = (uint32_t)(8 * XQ * gw + (lane >> 3)) * a.ld + loff;
   auto at = [&](int st) { return st < KB ? (uint32_t)st * kFp8Block : kOOB; };
-  // (addresses made anew for each load: kept, they cost the registers of a tile)
-  auto fresh = [](uint32_t v) {
-    asm volatile("" : "+v"(v));
-    return v;
-  };
   auto send_w = [&](uint8_t* dst, int half, int st) {
 #pragma unroll
     for (int q = 0; q < WQ; ++q)
@@ -478,7 +658,7 @@ __global__ __launch_bounds__(512, 2) void k_fp8_tile(LinearFp8Args a, int MT, in
 }
 
 template <bool PREC>
-static hipError_t launch_tile(const LinearFp8Args& a, hipStream_t s) {
+static hipError_t launch_tile_of(const LinearFp8Args& a, hipStream_t s) {
   typedef TileGeom<PREC> G;
   constexpr int TM = 16 * G::MI * G::WM, TN = 16 * G::NB * G::WN;
   const int MT = (a.n + TM - 1) / TM, NT = (a.N + TN - 1) / TN;
@@ -490,15 +670,266 @@ static hipError_t launch_tile(const LinearFp8Args& a, hipStream_t s) {
   return hipGetLastError();
 }
 
-hipError_t launch_linear_fp8(const LinearFp8Args& a, hipStream_t s) {
-  if (a.N > 64) return a.ybf16 ? launch_tile<false>(a, s) : launch_tile<true>(a, s);
-  const dim3 grid((a.n + 15) / 16, (a.N + 15) / 16);
-  KernelTimer timer("linear_fp8_few", s);
-  if (a.e8m0)
-    hipExtLaunchKernelGGL((k_fp8_few<true>), grid, dim3(kFewWaves * kWaveSize), 0, s, timer.start(), timer.stop(), 0, a);
-  else
-    hipExtLaunchKernelGGL((k_fp8_few<false>), grid, dim3(kFewWaves * kWaveSize), 0, s, timer.start(), timer.stop(), 0, a);
+// Rows between: a block of four waves owns 128 outputs x TN rows of x and one of S
+// parts of the column blocks; parts meet in k_fp8_join.  Exact products for every
+// output type, the values widened to bf16 between LDS and the matrix instructions.
+// Two or more blocks a compute unit hide each other's widening and reads.  A
+// step's operands go from memory straight to LDS while the step before is
+// multiplied, one barrier per step.
+template <int TN> struct MidGeom;
+template <> struct MidGeom<128> { static constexpr int WN = 2, MI = 2, NB = 2; };  // waves along x's rows, 32 x 32 tiles of a wave
+template <> struct MidGeom<64> { static constexpr int WN = 2, MI = 2, NB = 1; };
+template <> struct MidGeom<32> { static constexpr int WN = 1, MI = 1, NB = 1; };
+
+template <int TN, bool E8M0>
+__global__ __launch_bounds__(256, TN == 128 ? 2 : 3) void k_fp8_mid(LinearFp8Args a, int MT, int NT) {
+  typedef MidGeom<TN> G;
+  constexpr int T = 128, MI = G::MI, NB = G::NB, XQ = TN / 32;
+  __shared__ __attribute__((aligned(1024))) uint8_t w0[T * 128], w1[T * 128], x0[TN * 128], x1[TN * 128];
+  __shared__ float ring[8][TN + 1];  // scales of eight steps: of the tile's rows, and the weight's
+  const int tid = threadIdx.x, lane = tid & (kWaveSize - 1);
+  const int w = __builtin_amdgcn_readfirstlane(tid / kWaveSize);
+  const int wm = w / G::WN, wn = w % G::WN;
+  const int r32 = lane & 31, h = lane >> 5;
+  // blocks of one weight tile (and part) run on one XCD, one after the other
+  const int ix = blockIdx.x / 8, unit = (ix / NT) * 8 + blockIdx.x % 8;
+  if (unit >= MT * a.S) return;
+  const int part = unit / MT, c0 = (unit - part * MT) * T, t0 = ix % NT * TN;
+  const int KB = a.ld / kFp8Block;
+  const int first = (int)((int64_t)part * KB / a.S), last = (int)((int64_t)(part + 1) * KB / a.S);
+  const int nc = min(T, a.n - c0), nt = min(TN, a.N - t0);
+  const __amdgpu_buffer_rsrc_t rw = make_rsrc(a.wq + (size_t)c0 * a.ld, (uint32_t)nc * a.ld);
+  const __amdgpu_buffer_rsrc_t rx = make_rsrc(a.xq + (size_t)t0 * a.ld, (uint32_t)nt * a.ld);
+  // (LDS layout, rows and steps past the last: as k_fp8_tile)
+  const uint32_t loff = (uint32_t)((lane & 7) ^ (lane >> 3)) * 16u;
+  const uint32_t woff = (uint32_t)(32 * w + (lane >> 3)) * a.ld + loff, xoff = (uint32_t)(8 * XQ * w + (lane >> 3)) * a.ld + loff;
+  auto send = [&](uint8_t* sw, uint8_t* sx, int st) {
+    const uint32_t k = st < last ? (uint32_t)st * kFp8Block : kOOB;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) dma16(rw, sw + (4 * w + q) * 1024, fresh(woff) + (k + 8u * q * a.ld));
+#pragma unroll
+    for (int q = 0; q < XQ; ++q) dma16(rx, sx + (XQ * w + q) * 1024, fresh(xoff) + (k + 8u * q * a.ld));
+  };
+  // Scales, four steps at a time, into registers and a step later into LDS.
+  constexpr uint32_t SB = E8M0 ? 1 : 4;
+  const int srow = tid & (TN - 1);
+  const uint8_t* swp = static_cast<const uint8_t*>(a.ws) + (size_t)(c0 / kFp8Block) * KB * SB;
+  const uint8_t* sxp = static_cast<const uint8_t*>(a.xs) + (size_t)min(t0 + srow, a.N - 1) * KB * SB;
+  Fp8ScaleRun<E8M0> px, pw;
+  auto fetch_scales = [&](int st) {
+    px.load(sxp, st, KB);
+    pw.load(swp, st, KB);
+  };
+  auto put_scales = [&](int st) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      float* slot = ring[(scale_start(st, KB) + j) & 7];
+      slot[srow] = __uint_as_float(px.template get<false>(j));
+      slot[TN] = __uint_as_float(pw.template get<false>(j));
+    }
+  };
+
+  f32x16 acc[MI][NB];
+#pragma unroll
+  for (int i = 0; i < MI; ++i)
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[i][b][e] = 0.f;
+  // Lane (r32, h) holds pieces h, h + 2, h + 4, h + 6 of its row: 16 columns each,
+  // two instructions' depth of eight.
+  const uint32_t fslot = (uint32_t)(h ^ (r32 & 7)) * 16u;
+  const uint32_t abase = (uint32_t)(32 * MI * wm + r32) * 128u + fslot, bbase = (uint32_t)(32 * NB * wn + r32) * 128u + fslot;
+  auto step = [&](uint8_t* sw, uint8_t* sx, uint8_t* nw, uint8_t* nx, int st, auto fetch, auto put) {
+    wait_vm<0>();
+    if constexpr (decltype(put)::v) put_scales(st + 3);
+    wait_lds();
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    u32x4 fb[NB][4], fa[MI][4];
+    float sc[NB];
+    const float* ss = ring[st & 7];
+    const float swv = ss[TN];
+#pragma unroll
+    for (int b = 0; b < NB; ++b) sc[b] = ss[32 * NB * wn + 32 * b + r32];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+#pragma unroll
+      for (int b = 0; b < NB; ++b) fb[b][q] = *reinterpret_cast<const u32x4*>(sx + (fresh(bbase) ^ (32u * q)) + b * 4096);
+#pragma unroll
+      for (int i = 0; i < MI; ++i) fa[i][q] = *reinterpret_cast<const u32x4*>(sw + (fresh(abase) ^ (32u * q)) + i * 4096);
+    }
+    // (the loads behind the reads: a read behind a load waits for it)
+    __builtin_amdgcn_sched_barrier(0);
+    send(nw, nx, st + 1);
+    if constexpr (decltype(fetch)::v) fetch_scales(st + 4);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int b = 0; b < NB; ++b) sc[b] *= swv;
+    fp_bf16x8 xw[NB][8];
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+#pragma unroll
+      for (int b = 0; b < NB; ++b) {
+        xw[b][2 * q] = widen_part(fb[b][q], 0);
+        xw[b][2 * q + 1] = widen_part(fb[b][q], 1);
+      }
+#pragma unroll
+    for (int i = 0; i < MI; ++i) {
+      f32x16 p[NB];
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) p[b][e] = 0.f;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const fp_bf16x8 wv = widen_part(fa[i][k >> 1], k & 1);
+#pragma unroll
+        for (int b = 0; b < NB; ++b) p[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wv, xw[b][k], p[b], 0, 0, 0);
+      }
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[i][b][e] = fmaf(p[b][e], sc[b], acc[i][b][e]);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  constexpr Const<1> yes;
+  constexpr Const<0> none;
+  if (KB >= 4) {
+    fetch_scales(first);
+  } else {
+    px.load_few(sxp, KB);
+    pw.load_few(swp, KB);
+  }
+  send(w0, x0, first);
+  put_scales(first);
+  int st = first;
+  for (; st + 4 <= last; st += 4) {
+    step(w0, x0, w1, x1, st, yes, none);
+    step(w1, x1, w0, x0, st + 1, none, yes);
+    step(w0, x0, w1, x1, st + 2, none, none);
+    step(w1, x1, w0, x0, st + 3, none, none);
+  }
+  if (st < last) step(w0, x0, w1, x1, st, none, none);
+  if (st + 1 < last) step(w1, x1, w0, x0, st + 1, none, none);
+  if (st + 2 < last) step(w0, x0, w1, x1, st + 2, none, none);
+  wait_vm<0>();  // no load is on its way to LDS when the block ends
+
+  // D[i][j] sits in lane j + 32 ((i / 4) % 2), register i % 4 + 4 (i / 8).
+#pragma unroll
+  for (int b = 0; b < NB; ++b) {
+    const int t = t0 + 32 * NB * wn + 32 * b + r32;
+    if (t >= a.N) continue;
+#pragma unroll
+    for (int i = 0; i < MI; ++i)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int c = c0 + 32 * MI * wm + 32 * i + 8 * q + 4 * h;
+        const f32x4 v = {acc[i][b][4 * q], acc[i][b][4 * q + 1], acc[i][b][4 * q + 2], acc[i][b][4 * q + 3]};
+        if (c >= a.n) continue;
+        if (a.S > 1) {
+          *reinterpret_cast<f32x4*>(a.partial + ((size_t)part * a.N + t) * a.pitch + c) = v;
+        } else if ((a.n & 3) == 0) {
+          put_y4(a, (size_t)t * a.n + c, v);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (c + e < a.n) put_y(a, (size_t)t * a.n + c + e, v[e]);
+        }
+      }
+  }
+}
+
+// y = residual + the parts' sums, in part order.
+__global__ __launch_bounds__(256) void k_fp8_join(LinearFp8Args a) {
+  const uint32_t per = (uint32_t)a.pitch / 4, i = blockIdx.x * 256u + threadIdx.x;
+  if (i >= (uint32_t)a.N * per) return;
+  const uint32_t t = i / per, c = (i - t * per) * 4u;
+  const size_t stride = (size_t)a.N * a.pitch;
+  const float* p = a.partial + (size_t)t * a.pitch + c;
+  f32x4 v = *reinterpret_cast<const f32x4*>(p);
+#pragma unroll 4
+  for (int s = 1; s < a.S; ++s) v += *reinterpret_cast<const f32x4*>(p + s * stride);
+  const size_t at = (size_t)t * a.n + c;
+  if ((a.n & 3) == 0) {
+    put_y4(a, at, v);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (c + e < (uint32_t)a.n) put_y(a, at + e, v[e]);
+  }
+}
+
+template <int TN>
+static hipError_t launch_mid(const LinearFp8Args& a, hipStream_t s) {
+  const int MT = (a.n + 127) / 128, NT = (a.N + TN - 1) / TN;
+  const dim3 grid((unsigned)((MT * a.S + 7) / 8 * 8) * (unsigned)NT);
+  {
+    KernelTimer timer("linear_fp8_mid", s);
+    if (a.e8m0)
+      hipExtLaunchKernelGGL((k_fp8_mid<TN, true>), grid, dim3(256), 0, s, timer.start(), timer.stop(), 0, a, MT, NT);
+    else
+      hipExtLaunchKernelGGL((k_fp8_mid<TN, false>), grid, dim3(256), 0, s, timer.start(), timer.stop(), 0, a, MT, NT);
+  }
+  if (a.S > 1) {
+    KernelTimer timer("linear_fp8_join", s);
+    hipExtLaunchKernelGGL(k_fp8_join, dim3(((unsigned)a.N * (a.pitch / 4) + 255) / 256), dim3(256), 0, s, timer.start(), timer.stop(), 0, a);
+  }
   return hipGetLastError();
+}
+
+template <bool E8M0>
+static hipError_t launch_tile(const LinearFp8Args& a, hipStream_t s) { return a.ybf16 ? launch_tile_of<false>(a, s) : launch_tile_of<true>(a, s); }
+
+// How a call is run.
+enum LinearPath { kStreamPath, kSplitPath, kMidPath, kTilePath };
+struct LinearPlan { LinearPath path; int tn, S; };
+static LinearPlan linear_plan(int N, int n, int KB, bool bf16) {
+  const int steps = (KB + kStreamWaves - 1) / kStreamWaves;
+  if (N <= 16) return {steps <= 4 ? kStreamPath : kSplitPath, 16, 1};
+  if (N <= 32 && steps <= 2) return {kStreamPath, 32, 1};
+  const int tn = N <= 32 ? 32 : N <= 64 ? 64 : 128;
+  const int64_t MT = (n + 127) / 128, blocks = MT * ((N + tn - 1) / tn);
+  if (tn == 128) {
+    const int wide = bf16 ? 256 : 128;
+    const int64_t tiles = (int64_t)((n + 255) / 256) * ((N + wide - 1) / wide);
+    if (3 * ((tiles + 255) / 256) < 2 * ((blocks + 255) / 256)) return {kTilePath, wide, 1};
+  }
+  const int64_t want = tn == 128 ? 256 : 384;
+  int64_t S = (want + (tn == 128 ? blocks / 2 : 0)) / blocks;
+  const int most = KB / 6 > 1 ? KB / 6 : 1;
+  return {kMidPath, tn, (int)(S < 1 ? 1 : S > most ? most : S)};
+}
+
+static int partial_pitch(int n) { return (n + 3) / 4 * 4; }
+
+size_t linear_fp8_partial_bytes(int N, int n, int KB) {
+  size_t most = 0;
+  for (int bf16 = 0; bf16 < 2; ++bf16) {
+    const LinearPlan p = linear_plan(N, n, KB, bf16 != 0);
+    const size_t bytes = p.S > 1 ? (size_t)p.S * N * partial_pitch(n) * sizeof(float) : 0;
+    if (bytes > most) most = bytes;
+  }
+  return most;
+}
+
+hipError_t launch_linear_fp8(LinearFp8Args a, hipStream_t s) {
+  const int KB = a.ld / kFp8Block;
+  const LinearPlan p = linear_plan(a.N, a.n, KB, a.ybf16 != 0);
+  a.S = p.S;
+  a.pitch = partial_pitch(a.n);
+  switch (p.path) {
+    case kStreamPath:
+      if (p.tn == 32) return KB <= 16 ? launch_stream<1, 2>(a, s) : launch_stream<2, 2>(a, s);
+      if (KB <= 16) return launch_stream<1, 1>(a, s);
+      if (KB <= 32) return launch_stream<2, 1>(a, s);
+      return KB <= 48 ? launch_stream<3, 1>(a, s) : launch_stream<4, 1>(a, s);
+    case kSplitPath: return launch_split(a, s);
+    case kMidPath: return p.tn == 32 ? launch_mid<32>(a, s) : p.tn == 64 ? launch_mid<64>(a, s) : launch_mid<128>(a, s);
+    case kTilePath: return a.e8m0 ? launch_tile<true>(a, s) : launch_tile<false>(a, s);
+  }
+  return hipErrorInvalidValue;
 }
 
 }  // namespace cats

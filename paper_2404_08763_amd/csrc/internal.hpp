@@ -262,11 +262,16 @@ struct LinearFp8Args {
   void* y;               // [N x n] fp32 or bf16
   int N, n, ld;
   int e8m0, ybf16;
+  int S;                 // parts of the reduction (set by the launcher)
+  int pitch;             // n rounded up to 4
+  float* partial;        // [S x N x pitch]
 };
 hipError_t launch_quantize_fp8(const void* x, int bf16, int rows, int cols, int block_rows, const Fp8Out& o, hipStream_t s);
 hipError_t launch_silu_fp8(const void* gu, int bf16, int N, int m, float t, const Fp8Out& o, hipStream_t s);
 hipError_t launch_rmsnorm_fp8(const RmsnormFp8Args& a, int bf16, hipStream_t s);
-hipError_t launch_linear_fp8(const LinearFp8Args& a, hipStream_t s);
+hipError_t launch_linear_fp8(LinearFp8Args a, hipStream_t s);
+// Bytes of the partial sums that a call of that size may need (of either output type).
+size_t linear_fp8_partial_bytes(int N, int n, int KB);
 
 // Optional per-kernel timing (cats_timer_*): while the timer is enabled a
 // KernelTimer hands out a pair of HIP events that the launch (through
