@@ -11,16 +11,22 @@
 
 namespace cats {
 
-// Stores eight values of block (row, cb) and, from the group's first lane, its scale.
+// Stores a lane's eight values (times m) of block (row, cb), A the block's largest
+// finite one, and from the group's first lane its scale.
 template <bool E8M0>
-__device__ __forceinline__ void put_block(const Fp8Out& o, size_t row, int cb, int sub, uint32_t amax,
-                                          const float (&f)[8]) {
-  float inv;
-  const typename Fp8Scale<E8M0>::type s = Fp8Scale<E8M0>::stored(amax, inv);
-  const uint2 v = {fp8x4(f, inv), fp8x4(f + 4, inv)};
+__device__ __forceinline__ void put_block(const Fp8Out& o, size_t row, int cb, int sub, uint32_t A, const Fp8Factor& m,
+                                          float (&f)[8]) {
+  Fp8Factor k;
+  const typename Fp8Scale<E8M0>::type s = fp8_scale<E8M0, 8>(A, m, k, f);
+  const uint2 v = {fp8x4(f, k), fp8x4(f + 4, k)};
   *reinterpret_cast<uint2*>(o.q + row * o.ld + (size_t)cb * kFp8Block + sub * 8) = v;
   if (sub == 0) reinterpret_cast<typename Fp8Scale<E8M0>::type*>(o.scale)[row * (o.ld / kFp8Block) + cb] = s;
 }
+
+// SiLU with the reciprocal instruction (one fp32 step off) in place of a division,
+// whose instructions the gate's kernel would otherwise be bound by; the same
+// infinities, zeros and NaN.
+__device__ __forceinline__ float silu_fast(float z) { return z * __builtin_amdgcn_rcpf(1.0f + __expf(-z)); }
 
 // One group of 16 lanes per block of 128 columns of a row.  GATE: the row
 // holds m gate values, then m up values; h = SiLU(g) u where |SiLU(g)| is not below t.
@@ -38,26 +44,26 @@ __global__ __launch_bounds__(256) void k_fp8_rows(const T* __restrict__ x, int c
     load8(xr + cols, c, cols, u);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      const float v = silu(f[e]);
+      const float v = silu_fast(f[e]);
       f[e] = fabsf(v) < t ? 0.f : v * u[e];
     }
   }
-  put_block<E8M0>(o, row, cb, sub, max16(finite_max8(f)), f);
+  put_block<E8M0>(o, row, cb, sub, block_max<8>(f), Fp8Factor{1.f, 0.f}, f);
 }
 
-// One block of 256 threads per 128 x 128 weights, 64 of them per thread.
+// One block of 512 threads per 128 x 128 weights, 32 of them per thread.
 template <typename T, bool E8M0>
-__global__ __launch_bounds__(256) void k_fp8_tiles(const T* __restrict__ x, int rows, int cols, Fp8Out o) {
-  __shared__ uint32_t red[16];
+__global__ __launch_bounds__(512) void k_fp8_tiles(const T* __restrict__ x, int rows, int cols, Fp8Out o) {
+  constexpr int R = 4;  // rows of a thread
+  __shared__ uint32_t red[32];
   const int nb = o.ld / kFp8Block;
   const int rb = blockIdx.x / nb, cb = blockIdx.x - rb * nb;
   const int grp = threadIdx.x / 16, sub = threadIdx.x & 15, c = cb * kFp8Block + sub * 8;
   const int r0 = rb * kFp8Block + grp;
-  float f[8][8];
-  uint32_t a = 0;
+  float f[R][8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int r = r0 + 16 * i;
+  for (int i = 0; i < R; ++i) {
+    const int r = r0 + 32 * i;
     if (r < rows) {
       load8(x + (size_t)r * cols, c, cols, f[i]);
     } else {
@@ -65,19 +71,17 @@ __global__ __launch_bounds__(256) void k_fp8_tiles(const T* __restrict__ x, int 
       for (int e = 0; e < 8; ++e) f[i][e] = 0.f;
     }
   }
-#pragma unroll
-  for (int i = 0; i < 8; ++i) a = max(a, finite_max8(f[i]));
-  a = max16(a);
+  uint32_t a = block_max<8 * R>(&f[0][0]);
   if (sub == 0) red[grp] = a;
   __syncthreads();
-  a = max16(red[sub]);
-  float inv;
-  const typename Fp8Scale<E8M0>::type s = Fp8Scale<E8M0>::stored(a, inv);
+  a = max16(max(red[sub], red[sub + 16]));
+  Fp8Factor k;
+  const typename Fp8Scale<E8M0>::type s = fp8_scale<E8M0, 8 * R>(a, Fp8Factor{1.f, 0.f}, k, &f[0][0]);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int r = r0 + 16 * i;
+  for (int i = 0; i < R; ++i) {
+    const int r = r0 + 32 * i;
     if (r < rows)
-      *reinterpret_cast<uint2*>(o.q + (size_t)r * o.ld + c) = uint2{fp8x4(f[i], inv), fp8x4(f[i] + 4, inv)};
+      *reinterpret_cast<uint2*>(o.q + (size_t)r * o.ld + c) = uint2{fp8x4(f[i], k), fp8x4(f[i] + 4, k)};
   }
   if (threadIdx.x == 0) reinterpret_cast<typename Fp8Scale<E8M0>::type*>(o.scale)[(size_t)rb * nb + cb] = s;
 }
@@ -86,7 +90,7 @@ __global__ __launch_bounds__(256) void k_fp8_tiles(const T* __restrict__ x, int 
 // one read of x and the residual.
 template <typename T, bool E8M0, int NV>
 __global__ __launch_bounds__(1024) void k_rmsnorm_fp8(RmsnormFp8Args a) {
-  __shared__ float red[16];
+  __shared__ double red[16];
   const int d = a.d, tid = threadIdx.x, T0 = blockDim.x;
   const size_t row = blockIdx.x;
   const T* xr = static_cast<const T*>(a.x) + row * d;
@@ -111,29 +115,35 @@ __global__ __launch_bounds__(1024) void k_rmsnorm_fp8(RmsnormFp8Args a) {
   for (int i = 0; i < NV; ++i)
 #pragma unroll
     for (int e = 0; e < 8; ++e) ss = fmaf(f[i][e], f[i][e], ss);
-  ss = wave_sum(ss);
+  // sums of 16 lanes in fp32 (their roundings average out over the row's many), from
+  // there on in 64 bits
+  ss += dpp_f32<0xb1>(ss);
+  ss += dpp_f32<0x4e>(ss);
+  ss += dpp_f32<0x141>(ss);
+  ss += dpp_f32<0x140>(ss);
+  double sum = ((double)lane_f32(ss, 0) + lane_f32(ss, 16)) + ((double)lane_f32(ss, 32) + lane_f32(ss, 48));
   const int nw = T0 / kWaveSize;
   if (nw > 1) {
-    if ((tid & (kWaveSize - 1)) == 0) red[tid / kWaveSize] = ss;
+    if ((tid & (kWaveSize - 1)) == 0) red[tid / kWaveSize] = sum;
     __syncthreads();
-    ss = red[0];
-    for (int w = 1; w < nw; ++w) ss += red[w];
+    sum = red[0];
+    for (int w = 1; w < nw; ++w) sum += red[w];
   }
-  const float inv = 1.0f / sqrtf(ss / (float)d + a.eps);
+  const double r = 1.0 / sqrt(sum / d + (double)a.eps);
+  Fp8Factor m;
+  m.hi = (float)r;
+  m.lo = m.hi < __builtin_inff() ? (float)(r - m.hi) : 0.f;
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
     const int c = (tid + T0 * i) * 8;
     if (c >= a.o.ld) continue;
-    float y[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) y[e] = f[i][e] * inv;
     if (a.gain) {
       float g[8];
       load8(a.gain, c, d, g);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) y[e] *= g[e];
+      for (int e = 0; e < 8; ++e) f[i][e] *= g[e];
     }
-    put_block<E8M0>(a.o, row, c / kFp8Block, (c / 8) & 15, max16(finite_max8(y)), y);
+    put_block<E8M0>(a.o, row, c / kFp8Block, (c / 8) & 15, block_max<8>(f[i]), m, f[i]);
   }
 }
 
@@ -157,10 +167,10 @@ hipError_t tiles_launch(const void* x, int rows, int cols, const Fp8Out& o, hipS
   const dim3 grid((unsigned)((rows + kFp8Block - 1) / kFp8Block) * (unsigned)(o.ld / kFp8Block));
   KernelTimer timer("quantize_fp8_tiles", s);
   if (o.e8m0)
-    hipExtLaunchKernelGGL((k_fp8_tiles<T, true>), grid, dim3(256), 0, s, timer.start(), timer.stop(), 0,
+    hipExtLaunchKernelGGL((k_fp8_tiles<T, true>), grid, dim3(512), 0, s, timer.start(), timer.stop(), 0,
                           static_cast<const T*>(x), rows, cols, o);
   else
-    hipExtLaunchKernelGGL((k_fp8_tiles<T, false>), grid, dim3(256), 0, s, timer.start(), timer.stop(), 0,
+    hipExtLaunchKernelGGL((k_fp8_tiles<T, false>), grid, dim3(512), 0, s, timer.start(), timer.stop(), 0,
                           static_cast<const T*>(x), rows, cols, o);
   return hipGetLastError();
 }

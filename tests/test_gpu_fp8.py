@@ -124,6 +124,22 @@ def test_rmsnorm_special_rows():
         check_quantised(plain[ok], q[ok], s[ok], 1, NORM_DELTA)
 
 
+@pytest.mark.parametrize("stype", SCALES, ids=IDS)
+def test_rmsnorm_tiny_blocks(stype):
+    """Blocks of subnormal and nearly subnormal values beside ordinary ones: their
+    factor to e4m3 alone would overflow."""
+    say("rmsnorm tiny", stype)
+    x = torch.randn((4, 640), generator=gen(6))
+    x[:, 128:256] *= 1e-36
+    x[:, 256:384] *= 1e-39   # subnormal
+    x[:, 384:512] = 0.0
+    x[1:] *= 1e-3
+    x[2, 400] = 1e-45        # the least
+    x = x.to(DEV)
+    q, s = P.rmsnorm_fp8(x, eps=0.0, scale_dtype=stype)
+    check_quantised(_norm_ref(x, None, None, 0.0)[1], q, s, 1, NORM_DELTA)
+
+
 # ---- gate ------------------------------------------------------------------------
 
 # e^-z in fp32 with |z| <= 20: 20 * 1.5 + 4 half steps; the sum, quotient and product 4
