@@ -563,42 +563,51 @@ def _shape_is(t: torch.Tensor, shape: tuple, name: str) -> None:
         raise ValueError(f"{name} must be {list(shape)}, has shape {list(t.shape)}")
 
 
-def _here(name: str, t: torch.Tensor, dtype: torch.dtype, device: int) -> None:
-    """A contiguous tensor of that type on the current device, on whose stream
-    the call runs."""
+def _refuse(name: str, t: torch.Tensor, dtype: torch.dtype, device: int) -> None:
+    """Raises for a tensor that is not a contiguous one of that type on the
+    current device, on whose stream the call runs (the callers' own test of the
+    same costs a third of a call for each tensor)."""
     if not t.is_cuda:
         raise ValueError(f"{name} must be a device tensor")
     if t.dtype != dtype:
         raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
     if not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
-    if t.get_device() != device:
-        raise ValueError(f"{name} is on device {t.get_device()}, the current device is {device}")
+    raise ValueError(f"{name} is on device {t.get_device()}, the current device is {device}")
+
+
+_E4M3 = torch.float8_e4m3fn
 
 
 def _fp8_io(x: torch.Tensor, rows: int, cols: int, block_rows: int, scale_dtype: torch.dtype, out):
     """Checks a quantising call's input and returns its q and scale (out's, or
-    new ones) and the device they are on."""
-    if x.dtype is not torch.float32 and x.dtype is not torch.bfloat16:
-        raise ValueError(f"the input must be torch.float32 or torch.bfloat16, got {x.dtype}")
-    qs = (rows, fp8_ld(cols))
-    ss = (rows if block_rows == 1 else _blocks(rows), qs[1] // FP8_BLOCK)
+    new ones), the scale's type and the current device."""
+    xt = x.dtype
+    if xt is not torch.float32 and xt is not torch.bfloat16:
+        raise ValueError(f"the input must be torch.float32 or torch.bfloat16, got {xt}")
+    ld = (cols + FP8_BLOCK - 1) // FP8_BLOCK * FP8_BLOCK
+    qs, ss = (rows, ld), (rows if block_rows == 1 else _blocks(rows), ld // FP8_BLOCK)
     if out is not None:
         q, scale = out
-        _shape_is(q, qs, "q")
-        _shape_is(scale, ss, "scale")
+        if q.shape != qs:
+            _shape_is(q, qs, "q")
+        if scale.shape != ss:
+            _shape_is(scale, ss, "scale")
         scale_dtype = scale.dtype
-    _stype(scale_dtype)
+    st = _stype(scale_dtype)
     if not x.is_cuda:
         raise ValueError("the input must be a device tensor")
     if out is None:
-        q = torch.empty(qs, dtype=torch.float8_e4m3fn, device=x.device)
+        q = torch.empty(qs, dtype=_E4M3, device=x.device)
         scale = torch.empty(ss, dtype=scale_dtype, device=x.device)
     device = _device()
-    _here("the input", x, x.dtype, device)
-    _here("q", q, torch.float8_e4m3fn, device)
-    _here("scale", scale, scale.dtype, device)
-    return q, scale, device
+    if x.get_device() != device or not x.is_contiguous():
+        _refuse("the input", x, xt, device)
+    if q.dtype is not _E4M3 or q.get_device() != device or not q.is_contiguous():
+        _refuse("q", q, _E4M3, device)
+    if scale.get_device() != device or not scale.is_contiguous():
+        _refuse("scale", scale, scale_dtype, device)
+    return q, scale, st, device
 
 
 def _two_dims(x: torch.Tensor, name: str) -> tuple:
@@ -614,9 +623,9 @@ def quantize_fp8(x: torch.Tensor, block_rows: int = 1, scale_dtype: torch.dtype 
     rows, cols = _two_dims(x, "x")
     if block_rows not in (1, FP8_BLOCK):
         raise ValueError(f"block_rows must be 1 or {FP8_BLOCK}")
-    q, scale, _ = _fp8_io(x, rows, cols, block_rows, scale_dtype, out)
-    _check(raw().cats_quantize_fp8(x.data_ptr(), _wdtype(x.dtype), rows, cols, block_rows, _SCALE_TYPES[scale.dtype],
-                                   q.data_ptr(), scale.data_ptr(), _stream()))
+    q, scale, st, _ = _fp8_io(x, rows, cols, block_rows, scale_dtype, out)
+    _check(raw().cats_quantize_fp8(x.data_ptr(), _wdtype(x.dtype), rows, cols, block_rows, st, q.data_ptr(),
+                                   scale.data_ptr(), _stream()))
     return q, scale
 
 
@@ -627,13 +636,15 @@ def rmsnorm_fp8(x: torch.Tensor, residual: Optional[torch.Tensor] = None, gain: 
     fp32 or bf16, residual and sum_out [N, d] fp32 (sum_out receives s and may be
     the residual, or x if fp32), gain [d] fp32; a scale per row and 128 columns."""
     N, d = _two_dims(x, "x")
-    q, scale, device = _fp8_io(x, N, d, 1, scale_dtype, out)
+    q, scale, st, device = _fp8_io(x, N, d, 1, scale_dtype, out)
     for name, t, shape in (("residual", residual, (N, d)), ("gain", gain, (d,)), ("sum_out", sum_out, (N, d))):
         if t is not None:
-            _shape_is(t, shape, name)
-            _here(name, t, torch.float32, device)
-    _check(raw().cats_rmsnorm_fp8(x.data_ptr(), _wdtype(x.dtype), _ptr(residual), _ptr(gain), N, d, eps,
-                                  _SCALE_TYPES[scale.dtype], _ptr(sum_out), q.data_ptr(), scale.data_ptr(), _stream()))
+            if t.shape != shape:
+                _shape_is(t, shape, name)
+            if t.dtype is not torch.float32 or t.get_device() != device or not t.is_contiguous():
+                _refuse(name, t, torch.float32, device)
+    _check(raw().cats_rmsnorm_fp8(x.data_ptr(), _wdtype(x.dtype), _ptr(residual), _ptr(gain), N, d, eps, st,
+                                  _ptr(sum_out), q.data_ptr(), scale.data_ptr(), _stream()))
     return q, scale
 
 
@@ -645,9 +656,9 @@ def silu_mul_fp8(gate_up: torch.Tensor, t: float = 0.0, scale_dtype: torch.dtype
     if two_m % 2:
         raise ValueError(f"gate_up must be [N, 2 m], has {two_m} columns")
     m = two_m // 2
-    q, scale, _ = _fp8_io(gate_up, N, m, 1, scale_dtype, out)
-    _check(raw().cats_silu_mul_fp8(gate_up.data_ptr(), _wdtype(gate_up.dtype), N, m, t, _SCALE_TYPES[scale.dtype],
-                                   q.data_ptr(), scale.data_ptr(), _stream()))
+    q, scale, st, _ = _fp8_io(gate_up, N, m, 1, scale_dtype, out)
+    _check(raw().cats_silu_mul_fp8(gate_up.data_ptr(), _wdtype(gate_up.dtype), N, m, t, st, q.data_ptr(),
+                                   scale.data_ptr(), _stream()))
     return q, scale
 
 
@@ -668,9 +679,11 @@ def linear_fp8(xq: torch.Tensor, xs: torch.Tensor, wq: torch.Tensor, wscale: tor
     n, ldw = _two_dims(wq, "wq")
     if ld != ldw or ld % FP8_BLOCK:
         raise ValueError(f"xq and wq must have the same width, a multiple of {FP8_BLOCK}: got {ld} and {ldw}")
-    _shape_is(xs, (N, ld // FP8_BLOCK), "xs")
-    _shape_is(wscale, (_blocks(n), ld // FP8_BLOCK), "wscale")
-    st = _stype(xs.dtype)
+    nb = ld // FP8_BLOCK
+    _shape_is(xs, (N, nb), "xs")
+    _shape_is(wscale, (_blocks(n), nb), "wscale")
+    sdt = xs.dtype
+    st = _stype(sdt)
     if out is not None:
         _shape_is(out, (N, n), "out")
         dtype = out.dtype
@@ -682,17 +695,12 @@ def linear_fp8(xq: torch.Tensor, xs: torch.Tensor, wq: torch.Tensor, wscale: tor
     if out is None:
         out = torch.empty((N, n), dtype=dtype, device=xq.device)
     device = _device()
-    _here("xq", xq, torch.float8_e4m3fn, device)
-    _here("xs", xs, xs.dtype, device)
-    _here("wq", wq, torch.float8_e4m3fn, device)
-    _here("wscale", wscale, xs.dtype, device)
-    _here("out", out, dtype, device)
-    if residual is not None:
-        _here("residual", residual, dtype, device)
+    for name, t, dt in (("xq", xq, _E4M3), ("xs", xs, sdt), ("wq", wq, _E4M3), ("wscale", wscale, sdt),
+                        ("out", out, dtype), ("residual", residual, dtype), ("ws", ws, torch.uint8)):
+        if t is not None and (t.dtype is not dt or t.get_device() != device or not t.is_contiguous()):
+            _refuse(name, t, dt, device)
     if ws is None:
         ws = linear_fp8_workspace(N, n, ld, device=xq.device)
-    else:
-        _here("ws", ws, torch.uint8, device)
     _check(raw().cats_linear_fp8(xq.data_ptr(), xs.data_ptr(), N, wq.data_ptr(), wscale.data_ptr(), n, ld, st,
                                  _ptr(residual), out.data_ptr(), yt, ws.data_ptr(), ws.numel(), _stream()))
     return out
