@@ -576,9 +576,15 @@ __global__ __launch_bounds__(512, 2) void k_fp8_tile(LinearFp8Args a, int MT, in
     wait_lds();
     phase_end();
     send_w(next_whi, 1, st + 1);
-    multiply(none, half, Const<WQ>());
-    send_w(wlo, 0, st + 2);
-    multiply(half, all, Const<WQ>());
+    if constexpr (PREC) {
+      asm volatile("" ::: "memory");  // (in this order)
+      send_w(wlo, 0, st + 2);
+      multiply(none, all, Const<2 * WQ>());
+    } else {
+      multiply(none, half, Const<WQ>());
+      send_w(wlo, 0, st + 2);
+      multiply(half, all, Const<WQ>());
+    }
     wait_vm<2 * WQ + F>();
     phase_end();
   };
@@ -588,8 +594,12 @@ __global__ __launch_bounds__(512, 2) void k_fp8_tile(LinearFp8Args a, int MT, in
     wait_vm<0>();
     phase_end();
     send_x(xb, st + 2);
-    multiply(none, half, Const<XQ>());
-    multiply(half, all, none);
+    if constexpr (PREC) {
+      multiply(none, all, Const<XQ>());
+    } else {
+      multiply(none, half, Const<XQ>());
+      multiply(half, all, none);
+    }
     phase_end();
   };
   constexpr Const<1> yes;
