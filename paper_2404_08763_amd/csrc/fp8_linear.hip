@@ -1,6 +1,19 @@
 // Linear layer on e4m3 operands with a scale for each block:
 //   y[r, c] = residual[r, c] + sum_b xs[r, b] ws[c / 128, b] sum_{k in b} xq[r, k] wq[c, k]
-// with blocks b of 128 columns: just one matrix instruction's depth.
+// with column blocks b of 128.
+//
+// Weights are the matrix instructions' first operand and rows of x the second, so a
+// lane's results are fours of consecutive outputs of one row.  Which of a
+// block's columns sit in which lane does not matter as long as both operands agree.
+//
+// Precision.  The 8-bit matrix instructions cut each product at 2^-13 of the
+// power of two in the largest of its group of eight (measured: 256 * 256 beside
+// 2^2 gives 65536, beside 2^3 65544): 3e-5 to 5e-5 of the outputs in the mean
+// square on rows with outlier channels.  That is below bf16's rounding (2^-8) but
+// not fp32's, so they are used where y is bf16 and the products, not the reads,
+// bound the call (k_fp8_tile of bf16 outputs).  Elsewhere the values are widened
+// to bf16, which holds them exactly, on their way from the registers to the bf16
+// instructions, whose sums are exact to fp32.
 #include "fp8.hpp"
 #include "internal.hpp"
 #include "stream.hpp"
@@ -12,12 +25,12 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef __bf16 fp_bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 fp_bf16x2 __attribute__((ext_vector_type(2)));
 
-// Eight e4m3 values times 2^e (scale = 2^e) as bf16, which holds them exactly.
-__device__ __forceinline__ fp_bf16x8 widen8(uint32_t lo, uint32_t hi, float scale) {
-  const fp_bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false);
-  const fp_bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true);
-  const fp_bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false);
-  const fp_bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true);
+// Eight e4m3 values as bf16.
+__device__ __forceinline__ fp_bf16x8 widen8(uint32_t lo, uint32_t hi) {
+  const fp_bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.f, false);
+  const fp_bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.f, true);
+  const fp_bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.f, false);
+  const fp_bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.f, true);
   return fp_bf16x8{a.x, a.y, b.x, b.y, c.x, c.y, d.x, d.y};
 }
 
@@ -54,19 +67,9 @@ __device__ __forceinline__ uint32_t fresh(uint32_t v) {
   return v;
 }
 
-// A lane's 32 values of a column block.
-__device__ __forceinline__ void widen32(const u32x4 (&v)[2], fp_bf16x8 (&f)[4]) {
-#pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    f[2 * h] = widen8(v[h].x, v[h].y, 1.f);
-    f[2 * h + 1] = widen8(v[h].z, v[h].w, 1.f);
-  }
-}
-
-
 // Values 8 k .. 8 k + 7 of a lane's 16.
 __device__ __forceinline__ fp_bf16x8 widen_part(const u32x4& v, int k) {
-  return k ? widen8(v.z, v.w, 1.f) : widen8(v.x, v.y, 1.f);
+  return k ? widen8(v.z, v.w) : widen8(v.x, v.y);
 }
 
 __device__ __forceinline__ i32x8 join8(const u32x4& a, const u32x4& b) {
@@ -99,6 +102,18 @@ __device__ __forceinline__ void put_y4(const LinearFp8Args& a, size_t i, f32x4 v
   } else {
     if (a.residual) v += *reinterpret_cast<const f32x4*>(static_cast<const float*>(a.residual) + i);
     *reinterpret_cast<f32x4*>(static_cast<float*>(a.y) + i) = v;
+  }
+}
+
+// Outputs c .. c + 3 of row t, as far as there are any (c is a multiple of four).
+__device__ __forceinline__ void put_run(const LinearFp8Args& a, int t, int c, f32x4 v) {
+  const size_t at = (size_t)t * a.n + c;
+  if ((a.n & 3) == 0) {
+    if (c < a.n) put_y4(a, at, v);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (c + e < a.n) put_y(a, at + e, v[e]);
   }
 }
 
@@ -347,7 +362,7 @@ template <> struct Fp8ScaleRun<true> {
   }
 };
 
-constexpr int kTileGroup = 6;
+constexpr int kTileGroup = 6;  // (whole columns: 5% slower for 2048 rows 4096 -> 22016, 4 and 6 alike)
 
 // Many rows: a block of eight waves owns TM = 256 outputs x TN rows of x.
 //
@@ -364,8 +379,20 @@ constexpr int kTileGroup = 6;
 //   phase 2 s + 1  second group multiplies s, sends x of s + 2; first reads W0
 //                  and x of s + 1
 // so each part is overwritten once its readers are through with it, and has one
-// to three phases to arrive.
-template <bool PREC> struct TileGeom;
+// to three phases to arrive.  (All of a step's loads as its reads begin: 2048
+// rows 4096 -> 22016 in bf16 292 us with fp32 scales and 199 with E8M0, in place of
+// 211 and 162; one group of waves, multiplying and reading by turns in each: 352 and 256.)
+//
+// bf16 outputs: 256 x 256, the 8-bit instructions, one a tile and step, E8M0 scales
+// applied by them, fp32 ones on the vector ALUs, whose sums lie between the
+// products.  Bound by the matrix cores (0.6 of their time with E8M0), the sums and
+// what of the loads does not overlap: 4096 rows 14336 -> 4096 175 us, 2.7 PFLOP/s
+// (fp32 scales 226 us, 2.1), where the library's product of one scale for all takes 153.
+// EXACT, fp32 outputs: 256 x 128, the bf16 instructions; operands are widened in the
+// reading phase, under the other group's products (in the multiplying phase:
+// 410 us).  The same size 382 us, 1.26 PFLOP/s; the library's bf16 product, whose
+// operands have twice the bytes, takes 305.  Tiles of 32 x 32 had the same time or more.
+template <bool EXACT> struct TileGeom;
 template <> struct TileGeom<false> {
   static constexpr int WM = 2, WN = 4, MI = 8, NB = 4;  // waves, and 16 x 16 tiles of a wave
 };
@@ -373,14 +400,14 @@ template <> struct TileGeom<true> {
   static constexpr int WM = 4, WN = 2, MI = 4, NB = 4;
 };
 
-template <bool PREC, bool E8M0>
+template <bool EXACT, bool E8M0>
 __global__ __launch_bounds__(512, 2) void k_fp8_tile(LinearFp8Args a, int MT, int NT) {
-  typedef TileGeom<PREC> G;
+  typedef TileGeom<EXACT> G;
   constexpr int MI = G::MI, NB = G::NB;
   constexpr int TM = 16 * MI * G::WM, TN = 16 * NB * G::WN;
   static_assert(TM == 256 && MI * G::WM / 2 == 8, "a group's outputs are 128");
   constexpr int WQ = 4, XQ = TN / 32;  // 1 KB loads (8 rows) of a wave: of a half of the weights, of x
-  constexpr bool HW = E8M0 && !PREC;   // scales applied by the matrix instruction
+  constexpr bool HW = E8M0 && !EXACT;   // scales applied by the matrix instruction
   // one array per part in flight: the compiler then sees that a load into one
   // does not touch what is read from another
   __shared__ __attribute__((aligned(1024))) uint8_t wlo0[128 * 128], wlo1[128 * 128], whi0[128 * 128], whi1[128 * 128];
@@ -424,9 +451,9 @@ __global__ __launch_bounds__(512, 2) void k_fp8_tile(LinearFp8Args a, int MT, in
   };
 
   // Scales: each wave of the first group fetches those of 64 of the tile's rows and
-  // of the two weight blocks, four steps at a time (some lanes the same), and puts them into LDS a step later.  Not a load where they are used: its wait
-  // would be one for the operands under way too.  Where fewer than four steps are
-  // left, the last four of the row; where there are fewer, zeros past its end.
+  // of the two weight blocks, four steps at a time (some lanes the same), and puts
+  // them into LDS a step later.  Not a load where they are used: its wait would be
+  // one for the operands under way too (2048 rows 4096 -> 22016: 351 us against 292).
   constexpr uint32_t SB = E8M0 ? 1 : 4;
   typedef Fp8ScaleRun<E8M0> Run;
   const int wb = min(c0 / kFp8Block + (lane >> 5), (a.n - 1) / kFp8Block), srow = (64 * gw + lane) % TN;
@@ -441,13 +468,13 @@ __global__ __launch_bounds__(512, 2) void k_fp8_tile(LinearFp8Args a, int MT, in
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const int slot = (scale_start(st, KB) + j) & 7;
-      const uint32_t srow = fresh((uint32_t)(64 * gw + lane) % TN);
-      ring[slot][srow] = px.template get<HW>(j);
+      const uint32_t row = fresh((uint32_t)(64 * gw + lane) % TN);
+      ring[slot][row] = px.template get<HW>(j);
       ring[slot][TN + (lane >> 5)] = pw.template get<HW>(j);
     }
   };
   uint32_t xe[NB], we;
-  fp_bf16x8 xw[PREC ? NB : 1][4], ww[PREC ? MI : 1][4];
+  fp_bf16x8 xw[EXACT ? NB : 1][4], ww[EXACT ? MI : 1][4];
 
   f32x4 acc[MI][NB];
 #pragma unroll
@@ -475,11 +502,14 @@ __global__ __launch_bounds__(512, 2) void k_fp8_tile(LinearFp8Args a, int MT, in
       fa[i][0] = *reinterpret_cast<const u32x4*>(pa + i * 2048);
       fa[i][1] = *reinterpret_cast<const u32x4*>(pax + i * 2048);
     }
-    if constexpr (PREC) {
+    if constexpr (EXACT) {
 #pragma unroll
-      for (int b = 0; b < NB; ++b) widen32(fb[b], xw[b]);
+      for (int k = 0; k < 4; ++k) {
 #pragma unroll
-      for (int i = 0; i < MI; ++i) widen32(fa[i], ww[i]);
+        for (int b = 0; b < NB; ++b) xw[b][k] = widen_part(fb[b][k >> 1], k & 1);
+#pragma unroll
+        for (int i = 0; i < MI; ++i) ww[i][k] = widen_part(fa[i][k >> 1], k & 1);
+      }
     }
   };
   // The products of outputs I0 .. I1 - 1 of the wave's MI, and between them SENDS
@@ -492,7 +522,7 @@ __global__ __launch_bounds__(512, 2) void k_fp8_tile(LinearFp8Args a, int MT, in
 #pragma unroll
       for (int b = 0; b < NB; ++b) sc[b] = __uint_as_float(xe[b]) * __uint_as_float(we);
     }
-    if constexpr (PREC) {
+    if constexpr (EXACT) {
 #pragma unroll
       for (int i = I0; i < I1; ++i) {
         f32x4 p[NB];
@@ -575,8 +605,9 @@ __global__ __launch_bounds__(512, 2) void k_fp8_tile(LinearFp8Args a, int MT, in
     if constexpr (decltype(put)::v) put_scales(st + 3);
     wait_lds();
     phase_end();
+    __builtin_amdgcn_s_setprio(1);  // (products before the other group's widening: up to 3%)
     send_w(next_whi, 1, st + 1);
-    if constexpr (PREC) {
+    if constexpr (EXACT) {
       asm volatile("" ::: "memory");  // (in this order)
       send_w(wlo, 0, st + 2);
       multiply(none, all, Const<2 * WQ>());
@@ -585,6 +616,7 @@ __global__ __launch_bounds__(512, 2) void k_fp8_tile(LinearFp8Args a, int MT, in
       send_w(wlo, 0, st + 2);
       multiply(half, all, Const<WQ>());
     }
+    __builtin_amdgcn_s_setprio(0);
     wait_vm<2 * WQ + F>();
     phase_end();
   };
@@ -593,13 +625,15 @@ __global__ __launch_bounds__(512, 2) void k_fp8_tile(LinearFp8Args a, int MT, in
     wait_lds();
     wait_vm<0>();
     phase_end();
+    __builtin_amdgcn_s_setprio(1);
     send_x(xb, st + 2);
-    if constexpr (PREC) {
+    if constexpr (EXACT) {
       multiply(none, all, Const<XQ>());
     } else {
       multiply(none, half, Const<XQ>());
       multiply(half, all, none);
     }
+    __builtin_amdgcn_s_setprio(0);
     phase_end();
   };
   constexpr Const<1> yes;
@@ -655,37 +689,32 @@ __global__ __launch_bounds__(512, 2) void k_fp8_tile(LinearFp8Args a, int MT, in
 #pragma unroll
     for (int i = 0; i < MI; ++i) {
       const int c = c0 + 16 * MI * wm + 16 * i + 4 * g;
-      const size_t at = (size_t)t * a.n + c;
-      if ((a.n & 3) == 0) {
-        if (c < a.n) put_y4(a, at, acc[i][b]);
-      } else {
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (c + e < a.n) put_y(a, at + e, acc[i][b][e]);
-      }
+      put_run(a, t, c, acc[i][b]);
     }
   }
 }
 
-template <bool PREC>
+template <bool EXACT>
 static hipError_t launch_tile_of(const LinearFp8Args& a, hipStream_t s) {
-  typedef TileGeom<PREC> G;
+  typedef TileGeom<EXACT> G;
   constexpr int TM = 16 * G::MI * G::WM, TN = 16 * G::NB * G::WN;
   const int MT = (a.n + TM - 1) / TM, NT = (a.N + TN - 1) / TN;
-  KernelTimer timer(PREC ? "linear_fp8_tile_f32" : "linear_fp8_tile", s);
+  KernelTimer timer(EXACT ? "linear_fp8_tile_f32" : "linear_fp8_tile", s);
   if (a.e8m0)
-    hipExtLaunchKernelGGL((k_fp8_tile<PREC, true>), dim3(MT * NT), dim3(512), 0, s, timer.start(), timer.stop(), 0, a, MT, NT);
+    hipExtLaunchKernelGGL((k_fp8_tile<EXACT, true>), dim3(MT * NT), dim3(512), 0, s, timer.start(), timer.stop(), 0, a, MT, NT);
   else
-    hipExtLaunchKernelGGL((k_fp8_tile<PREC, false>), dim3(MT * NT), dim3(512), 0, s, timer.start(), timer.stop(), 0, a, MT, NT);
+    hipExtLaunchKernelGGL((k_fp8_tile<EXACT, false>), dim3(MT * NT), dim3(512), 0, s, timer.start(), timer.stop(), 0, a, MT, NT);
   return hipGetLastError();
 }
 
 // Rows between: a block of four waves owns 128 outputs x TN rows of x and one of S
-// parts of the column blocks; parts meet in k_fp8_join.  Exact products for every
-// output type, the values widened to bf16 between LDS and the matrix instructions.
-// Two or more blocks a compute unit hide each other's widening and reads.  A
-// step's operands go from memory straight to LDS while the step before is
-// multiplied, one barrier per step.
+// parts of the column blocks; parts meet in k_fp8_join.  Values are widened
+// between LDS and the bf16 instructions for every output type.  A step's operands
+// go from memory straight to LDS while the step before is multiplied, one barrier
+// a step.  Bound by a step's chain of reads, widening and products (1.2 us of a
+// lone block of 128 x 128, 1.0 each of two on a compute unit) where there are few
+// steps, by the parts' traffic and the second launch where there are many parts:
+// 256 rows 4096 -> 4096 22 us, 101 rows 7001 -> 2857 17.5.
 template <int TN> struct MidGeom;
 template <> struct MidGeom<128> { static constexpr int WN = 2, MI = 2, NB = 2; };  // waves along x's rows, 32 x 32 tiles of a wave
 template <> struct MidGeom<64> { static constexpr int WN = 2, MI = 2, NB = 1; };
@@ -840,12 +869,8 @@ __global__ __launch_bounds__(256, TN == 128 ? 2 : 3) void k_fp8_mid(LinearFp8Arg
         if (c >= a.n) continue;
         if (a.S > 1) {
           *reinterpret_cast<f32x4*>(a.partial + ((size_t)part * a.N + t) * a.pitch + c) = v;
-        } else if ((a.n & 3) == 0) {
-          put_y4(a, (size_t)t * a.n + c, v);
         } else {
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (c + e < a.n) put_y(a, (size_t)t * a.n + c + e, v[e]);
+          put_run(a, t, c, v);
         }
       }
   }
@@ -861,14 +886,7 @@ __global__ __launch_bounds__(256) void k_fp8_join(LinearFp8Args a) {
   f32x4 v = *reinterpret_cast<const f32x4*>(p);
 #pragma unroll 4
   for (int s = 1; s < a.S; ++s) v += *reinterpret_cast<const f32x4*>(p + s * stride);
-  const size_t at = (size_t)t * a.n + c;
-  if ((a.n & 3) == 0) {
-    put_y4(a, at, v);
-  } else {
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-      if (c + e < (uint32_t)a.n) put_y(a, at + e, v[e]);
-  }
+  put_run(a, (int)t, (int)c, v);
 }
 
 template <int TN>
@@ -894,30 +912,55 @@ static hipError_t launch_tile(const LinearFp8Args& a, hipStream_t s) { return a.
 
 // How a call is run.
 enum LinearPath { kStreamPath, kSplitPath, kMidPath, kTilePath };
-struct LinearPlan { LinearPath path; int tn, S; };
-static LinearPlan linear_plan(int N, int n, int KB, bool bf16) {
-  const int steps = (KB + kStreamWaves - 1) / kStreamWaves;
-  if (N <= 16) return {steps <= 4 ? kStreamPath : kSplitPath, 16, 1};
-  if (N <= 32 && steps <= 2) return {kStreamPath, 32, 1};
-  const int tn = N <= 32 ? 32 : N <= 64 ? 64 : 128;
-  const int64_t MT = (n + 127) / 128, blocks = MT * ((N + tn - 1) / tn);
-  if (tn == 128) {
+struct LinearPlan {
+  LinearPath path;
+  int rows;  // of x, of a tile (stream and mid)
+  int S;     // parts of the reduction
+};
+
+// us of a column block's step, from the sizes below over their steps: of a round of
+// 256 tiles (one a compute unit) of the two-group kernel, and of the 128 x 128 kernel, whose
+// blocks of one compute unit overlap.
+constexpr int kTileStepF32 = 172, kTileStepE8m0 = 160, kTileStep = 210;  // in 1/100: fp32 outputs, bf16 by type of scale
+constexpr int kMidStepOne = 127, kMidStepEach = 103;
+
+// us a call, weights rotated so that they come from memory:
+// Up to 16 rows, and up to 32 of no more than 32 column blocks: the streaming kernel
+// (32 rows 4096 -> 22016 22 against 26 of the 128 x 32 tiles; 1 row 8192 -> 28672 46, split
+// 50), unless a wave had more than four column blocks of x to keep.
+// Above: 128 outputs x 32, 64 or 128 rows, in parts while there are fewer blocks than
+// compute units take (256, or 384 of the small tiles, of which three fit one), but of
+// six column blocks at least (101 rows 7001 -> 2857, fp32: 4 / 8 / 16 parts 20 / 18 / 21;
+// 256 rows 4096 -> 4096: 2 / 4 / 8 / 12 parts 27 / 22 / 26 / 31; 64 rows 11008 -> 4096: 4 / 8 /
+// 16 / 20 parts 29 / 21 / 22 / 26; 32 rows 4096 -> 22016, 172 tiles: 1 / 2 / 3 parts 35 / 26 / 29).
+// The two-group kernel, with its larger tiles, once they fill the compute units
+// better (two-group / 128 x 128: 512 rows 4096 -> 22016, bf16 71 / 102, fp32 111 / 104; 256
+// rows, bf16 with fp32 scales 70 / 62, with E8M0 52 / 62; 2048 rows 4096 -> 4096, fp32 60 / 74;
+// 1024 rows 11008 -> 4096, fp32 128 / 102; 4096 rows 512 -> 4096, bf16 21 / 34).
+static LinearPlan linear_plan(int N, int n, int KB, bool bf16, bool e8m0) {
+  const int each = (KB + kStreamWaves - 1) / kStreamWaves;  // column blocks of a wave
+  if (N <= 16) return {each <= 4 ? kStreamPath : kSplitPath, 16, 1};
+  if (N <= 32 && each <= 2) return {kStreamPath, 32, 1};
+  const int rows = N <= 32 ? 32 : N <= 64 ? 64 : 128;
+  const int64_t blocks = (int64_t)((n + 127) / 128) * ((N + rows - 1) / rows);
+  const int64_t rounds = (blocks + 255) / 256;
+  if (rows == 128) {
     const int wide = bf16 ? 256 : 128;
     const int64_t tiles = (int64_t)((n + 255) / 256) * ((N + wide - 1) / wide);
-    if (3 * ((tiles + 255) / 256) < 2 * ((blocks + 255) / 256)) return {kTilePath, wide, 1};
+    const int step = !bf16 ? kTileStepF32 : e8m0 ? kTileStepE8m0 : kTileStep;
+    if (step * ((tiles + 255) / 256) < (rounds == 1 ? kMidStepOne : kMidStepEach * rounds)) return {kTilePath, wide, 1};
   }
-  const int64_t want = tn == 128 ? 256 : 384;
-  int64_t S = (want + (tn == 128 ? blocks / 2 : 0)) / blocks;
+  const int64_t S = rows == 128 ? (256 + blocks / 2) / blocks : 384 / blocks;
   const int most = KB / 6 > 1 ? KB / 6 : 1;
-  return {kMidPath, tn, (int)(S < 1 ? 1 : S > most ? most : S)};
+  return {kMidPath, rows, (int)(S < 1 ? 1 : S > most ? most : S)};
 }
 
 static int partial_pitch(int n) { return (n + 3) / 4 * 4; }
 
 size_t linear_fp8_partial_bytes(int N, int n, int KB) {
   size_t most = 0;
-  for (int bf16 = 0; bf16 < 2; ++bf16) {
-    const LinearPlan p = linear_plan(N, n, KB, bf16 != 0);
+  for (int v = 0; v < 4; ++v) {
+    const LinearPlan p = linear_plan(N, n, KB, (v & 1) != 0, (v & 2) != 0);
     const size_t bytes = p.S > 1 ? (size_t)p.S * N * partial_pitch(n) * sizeof(float) : 0;
     if (bytes > most) most = bytes;
   }
@@ -926,17 +969,17 @@ size_t linear_fp8_partial_bytes(int N, int n, int KB) {
 
 hipError_t launch_linear_fp8(LinearFp8Args a, hipStream_t s) {
   const int KB = a.ld / kFp8Block;
-  const LinearPlan p = linear_plan(a.N, a.n, KB, a.ybf16 != 0);
+  const LinearPlan p = linear_plan(a.N, a.n, KB, a.ybf16 != 0, a.e8m0 != 0);
   a.S = p.S;
   a.pitch = partial_pitch(a.n);
   switch (p.path) {
     case kStreamPath:
-      if (p.tn == 32) return KB <= 16 ? launch_stream<1, 2>(a, s) : launch_stream<2, 2>(a, s);
+      if (p.rows == 32) return KB <= 16 ? launch_stream<1, 2>(a, s) : launch_stream<2, 2>(a, s);
       if (KB <= 16) return launch_stream<1, 1>(a, s);
       if (KB <= 32) return launch_stream<2, 1>(a, s);
       return KB <= 48 ? launch_stream<3, 1>(a, s) : launch_stream<4, 1>(a, s);
     case kSplitPath: return launch_split(a, s);
-    case kMidPath: return p.tn == 32 ? launch_mid<32>(a, s) : p.tn == 64 ? launch_mid<64>(a, s) : launch_mid<128>(a, s);
+    case kMidPath: return p.rows == 32 ? launch_mid<32>(a, s) : p.rows == 64 ? launch_mid<64>(a, s) : launch_mid<128>(a, s);
     case kTilePath: return a.e8m0 ? launch_tile<true>(a, s) : launch_tile<false>(a, s);
   }
   return hipErrorInvalidValue;

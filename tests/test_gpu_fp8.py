@@ -6,7 +6,7 @@ import paper_2404_08763_amd as P
 from paper_2404_08763_amd import workloads as W
 
 from fp8_util import BLOCK, E8M0, F32, U, check_linear, check_quantised, gen, ld_of, linear_ref, quantised
-from gpu_util import say
+from gpu_util import kernels_of, say
 
 pytestmark = pytest.mark.gpu
 
@@ -187,7 +187,8 @@ def _operands(N, n, k, stype, seed=0):
 LINEAR = [(1, 1, 1), (1, 16, 128), (1, 6144, 4096), (2, 130, 129), (5, 40, 7001), (16, 257, 512), (17, 129, 1000), (31, 2000, 257),
           (33, 257, 384), (48, 1000, 3000), (64, 512, 2048), (65, 4096, 640), (100, 300, 2000), (128, 513, 1152),
           (129, 4097, 128), (255, 640, 4096), (257, 1000, 4224), (300, 2048, 8320), (512, 1024, 256), (700, 3001, 1000),
-          (1024, 2048, 384), (2000, 4100, 300)]
+          (1024, 2048, 384), (2000, 4100, 300), (1537, 4097, 1153), (1537, 4100, 128), (1540, 4100, 200), (1537, 4097, 300),
+          (1537, 4100, 640), (8, 300, 9000), (16, 100, 8192), (20, 515, 5000), (32, 4097, 4096)]
 
 
 @pytest.mark.parametrize("stype", SCALES, ids=IDS)
@@ -213,6 +214,29 @@ def test_linear(N, n, k, stype):
     assert _same(P.linear_fp8(xq, xs, wq, ws), y), "bit for bit again"
 
 
+@pytest.mark.parametrize("N,n,k,dtype,stype,kernels", [
+    (1, 6144, 4096, torch.float32, F32, {"linear_fp8_stream"}),
+    (16, 100, 8192, torch.float32, E8M0, {"linear_fp8_stream"}),
+    (32, 4097, 4096, torch.bfloat16, F32, {"linear_fp8_stream"}),
+    (8, 300, 9000, torch.float32, F32, {"linear_fp8_split"}),
+    (20, 515, 5000, torch.float32, F32, {"linear_fp8_mid", "linear_fp8_join"}),
+    (64, 512, 2048, torch.float32, E8M0, {"linear_fp8_mid", "linear_fp8_join"}),
+    (100, 300, 2000, torch.bfloat16, F32, {"linear_fp8_mid", "linear_fp8_join"}),
+    (1024, 2048, 384, torch.float32, F32, {"linear_fp8_mid"}),
+    (700, 3001, 1000, torch.float32, F32, {"linear_fp8_mid"}),
+    (1537, 4097, 1153, torch.float32, F32, {"linear_fp8_tile_f32"}),
+    (1537, 4097, 1153, torch.float32, E8M0, {"linear_fp8_tile_f32"}),
+    (2000, 4100, 300, torch.bfloat16, F32, {"linear_fp8_tile"}),
+    (2000, 4100, 300, torch.bfloat16, E8M0, {"linear_fp8_tile"}),
+])
+def test_every_kernel_is_tested(N, n, k, dtype, stype, kernels):
+    """Sizes of the tests above reach each kernel of the product."""
+    say("path", N, n, k, dtype, stype)
+    ops = _operands(N, n, k, stype)
+    assert (N, n, k) in LINEAR
+    assert kernels_of(lambda: P.linear_fp8(*ops, dtype=dtype)) == kernels
+
+
 def _guarded(shape, dtype):
     """A tensor between two stretches of a known pattern, and a check of them."""
     count = 1
@@ -225,7 +249,8 @@ def _guarded(shape, dtype):
 
 
 @pytest.mark.parametrize("stype", SCALES, ids=IDS)
-@pytest.mark.parametrize("N,n,k", [(1, 33, 200), (19, 130, 128), (130, 259, 500), (300, 513, 1000)])
+@pytest.mark.parametrize("N,n,k", [(1, 33, 200), (7, 35, 9000), (19, 130, 128), (40, 131, 3000), (130, 259, 500), (300, 513, 1000),
+                                   (1537, 4097, 300)])
 def test_writes_stay_inside(N, n, k, stype):
     say("guards", N, n, k, stype)
     xq, xs, wq, ws = _operands(N, n, k, stype)
@@ -236,6 +261,9 @@ def test_writes_stay_inside(N, n, k, stype):
     scratch, ok_ws = _guarded((need,), torch.uint8)
     P.linear_fp8(xq, xs, wq, ws, out=y, ws=scratch)
     assert ok() and ok_ws()
+    y16, ok16 = _guarded((N, n), torch.bfloat16)
+    P.linear_fp8(xq, xs, wq, ws, out=y16, ws=scratch)
+    assert ok16() and ok_ws()
     q, ok_q = _guarded((N, ld_of(k)), torch.float8_e4m3fn)
     s, ok_s = _guarded((N, ld_of(k) // BLOCK), stype)
     x = _rows(N, k, 1)
@@ -252,19 +280,23 @@ def test_writes_stay_inside(N, n, k, stype):
     assert ok_q() and ok_s()
 
 
-@pytest.mark.parametrize("N", [1, 40, 300])
-def test_linear_any_fp32_scale(N):
+BOTH = pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["y32", "y16"])
+
+
+@BOTH
+@pytest.mark.parametrize("N", [1, 40, 300, 12000, 30000])
+def test_linear_any_fp32_scale(N, dtype):
     """Scales a user brings: negative, zero, any; a NaN or infinite scale reaches its rows alone."""
-    say("linear scales", N)
+    say("linear scales", N, dtype)
     xq, xs, wq, ws = _operands(N, 300, 512, F32)
     xs = xs * torch.randn(xs.shape, generator=gen(1)).to(DEV)
     ws = ws * torch.randn(ws.shape, generator=gen(2)).to(DEV)
     xs[:, 1] = 0.0
     ref, mag = linear_ref(xq, xs, wq, ws)
-    check_linear(P.linear_fp8(xq, xs, wq, ws), ref, mag, 512)
+    check_linear(P.linear_fp8(xq, xs, wq, ws, dtype=dtype), ref, mag, 512)
     xs[N - 1, 2] = float("nan")
     ws[1, 0] = float("inf")
-    y = P.linear_fp8(xq, xs, wq, ws)
+    y = P.linear_fp8(xq, xs, wq, ws, dtype=dtype)
     assert torch.isnan(y[N - 1]).all()
     assert not torch.isfinite(y[:, 128:256]).any()
     if N > 1:
@@ -272,33 +304,35 @@ def test_linear_any_fp32_scale(N):
         check_linear(y[:-1, 256:], ref[:-1, 256:], mag[:-1, 256:], 512)
 
 
-@pytest.mark.parametrize("N", [1, 40, 300])
-def test_linear_e8m0_range(N):
+@BOTH
+@pytest.mark.parametrize("N", [1, 40, 300, 20000])
+def test_linear_e8m0_range(N, dtype):
     """Scales whose product is ordinary though each is extreme, and a NaN scale."""
-    say("linear e8m0", N)
+    say("linear e8m0", N, dtype)
     xq, xs, wq, ws = _operands(N, 200, 384, E8M0)
     xs.view(torch.uint8)[:, 0] = 0      # 2^-127
     ws.view(torch.uint8)[:, 0] = 254    # 2^127
     xs.view(torch.uint8)[:, 2] = 240
     ws.view(torch.uint8)[:, 2] = 10
     ref, mag = linear_ref(xq, xs, wq, ws)
-    check_linear(P.linear_fp8(xq, xs, wq, ws), ref, mag, 384)
+    check_linear(P.linear_fp8(xq, xs, wq, ws, dtype=dtype), ref, mag, 384)
     xs.view(torch.uint8)[0, 1] = 255
-    y = P.linear_fp8(xq, xs, wq, ws)
+    y = P.linear_fp8(xq, xs, wq, ws, dtype=dtype)
     assert torch.isnan(y[0]).all()
     if N > 1:
         check_linear(y[1:], ref[1:], mag[1:], 384)
 
 
 @pytest.mark.parametrize("stype", SCALES, ids=IDS)
-@pytest.mark.parametrize("N", [3, 50, 260])
-def test_linear_nan_in_q_stays_in_its_row(N, stype):
-    say("linear nan", N, stype)
+@BOTH
+@pytest.mark.parametrize("N", [3, 50, 260, 40000])
+def test_linear_nan_in_q_stays_in_its_row(N, stype, dtype):
+    say("linear nan", N, stype, dtype)
     xq, xs, wq, ws = _operands(N, 140, 640, stype)
     ref, mag = linear_ref(xq, xs, wq, ws)
     xq.view(torch.uint8)[1, 600] = 0x7f
     wq.view(torch.uint8)[139, 0] = 0xff
-    y = P.linear_fp8(xq, xs, wq, ws)
+    y = P.linear_fp8(xq, xs, wq, ws, dtype=dtype)
     assert torch.isnan(y[1]).all() and torch.isnan(y[:, 139]).all()
     keep = [i for i in range(N) if i != 1]
     check_linear(y[keep][:, :139], ref[keep][:, :139], mag[keep][:, :139], 640)
