@@ -20,7 +20,7 @@
  *    "host" host memory.  `stream` is a hipStream_t (NULL = the default
  *    stream of the current device); every device pointer must belong to the
  *    current device.
- *  - The forward, dense, pack and rmsnorm calls only enqueue work on
+ *  - The forward, dense, pack, rmsnorm and 8-bit calls only enqueue work on
  *    `stream` (no host synchronisation, no allocation).  Outputs are valid
  *    once the stream reaches that point.  The two calibration calls
  *    synchronise `stream` because they return t on the host.
@@ -349,8 +349,8 @@ cats_status cats_rmsnorm(const float* x, float* xn, int32_t B, int32_t d, float 
  * The calls that write such matrices take, with a the block's largest finite
  * magnitude, the scale a / 448 in fp32 (2^-126 if that is less), or the
  * smallest 2^e with a <= 448 * 2^e and e >= -126, and 1 where a is 0; q is the
- * nearest e4m3 value of element / scale (ties to even; the fp32 quotient may be
- * off by 1.5 of its last bits).  An infinite or NaN element becomes e4m3's NaN;
+ * nearest e4m3 value of element / scale, its quotient computed to more than fp32
+ * (to fp32 where the scale is 2^-126; ties to even).  An infinite or NaN element becomes e4m3's NaN;
  * the block's other elements are what they are without it.
  * All four calls are enqueue only and may be captured in a graph. */
 #define CATS_FP8_BLOCK 128
@@ -389,11 +389,12 @@ cats_status cats_rmsnorm_fp8(const void* x, int32_t dtype, const float* residual
  * row's m gate values g = x W_gate, then its m up values u = x W_up; fp32 or bf16)
  *   v = SiLU(g),  h = v * u where |v| >= t, else 0,  q, scale = quantise(h)
  * with one scale per row and CATS_FP8_BLOCK neurons.  t >= 0 as in
- * cats_mlp_forward (NaN v is kept; t = 0 keeps every neuron, t = +inf none). */
+ * cats_mlp_forward (NaN v is kept; t = 0 keeps every neuron, t = +inf no
+ * finite one).  SiLU(g) of less than 1.2e-36 may be 0. */
 cats_status cats_silu_mul_fp8(const void* gate_up, int32_t dtype, int32_t N, int32_t m, float t, int32_t stype, void* q,
                               void* scale, void* stream);
 
-/* Linear layer on 8-bit operands, sums in fp32:
+/* Linear layer on 8-bit operands:
  *   y[r, j] = residual[r, j] + sum_b xs[r, b] wscale[j / 128, b] sum_{c in block b} xq[r, c] wq[j, c]
  *   xq, xs      rows of x: [N x ld], block_rows 1
  *   wq, wscale  the weight, row j = output j: [n x ld], block_rows CATS_FP8_BLOCK
@@ -401,7 +402,11 @@ cats_status cats_silu_mul_fp8(const void* gate_up, int32_t dtype, int32_t N, int
  *   residual    dev [N x n] of ydtype or NULL;  y dev [N x n], CATS_F32 or
  *               CATS_BF16 (rounded once, after the residual).  y may be the
  *               residual, and overlaps nothing else.
- * xq, wq, y and residual 16-byte aligned.  NaN in q or a scale makes NaN of the
+ * For fp32 y the products are exact and summed in fp32.  For bf16 y and many
+ * rows the 8-bit matrix instructions multiply: they cut each product at 2^-13 of
+ * the power of two in the largest of its group of eight columns, below bf16's
+ * rounding of sums whose terms do not cancel.
+ * xq, wq, y and residual 16-byte aligned; ws overlaps nothing.  NaN in q or a scale makes NaN of the
  * outputs it reaches; scales may be any number of their type whose product of
  * two, which is formed first, is in fp32's range.  1 <= N, n <=
  * CATS_MAX_FP8_ROWS, 1 <= k <= CATS_MAX_FP8_COLS.  Workspace:

@@ -166,6 +166,11 @@ cats_status cats_linear_fp8(const void* xq, const void* xs, int32_t N, const voi
   if (!ws) return fail(CATS_ERR_WORKSPACE, "workspace is NULL");
   if (!aligned(ws, kWsAlign)) return fail(CATS_ERR_ALIGN, "workspace must be 256-byte aligned");
   if (ws_bytes < need) return fail(CATS_ERR_WORKSPACE, "workspace has %zu bytes, needs %zu", ws_bytes, need);
+  if (overlap(ws, need, xq, (size_t)N * ld) || overlap(ws, need, wq, (size_t)n * ld) || overlap(ws, need, y, ny) ||
+      overlap(ws, need, xs, (size_t)N * blocks_of(k) * scale_bytes(stype)) ||
+      overlap(ws, need, wscale, blocks_of(n) * blocks_of(k) * scale_bytes(stype)) ||
+      (residual && overlap(ws, need, residual, ny)))
+    return fail(CATS_ERR_RANGE, "the workspace must not overlap any operand");
   cats::LinearFp8Args a{};
   a.xq = static_cast<const uint8_t*>(xq);
   a.xs = xs;

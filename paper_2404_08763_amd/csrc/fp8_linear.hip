@@ -714,7 +714,7 @@ __global__ __launch_bounds__(512, 2) void k_fp8_tile(LinearFp8Args a, int MT, in
 }
 
 template <bool EXACT>
-static hipError_t launch_tile_of(const LinearFp8Args& a, hipStream_t s) {
+static hipError_t launch_tile(const LinearFp8Args& a, hipStream_t s) {
   typedef TileGeom<EXACT> G;
   constexpr int TM = 16 * G::MI * G::WM, TN = 16 * G::NB * G::WN;
   const int MT = (a.n + TM - 1) / TM, NT = (a.N + TN - 1) / TN;
@@ -931,9 +931,6 @@ static hipError_t launch_mid(const LinearFp8Args& a, hipStream_t s) {
   return hipGetLastError();
 }
 
-template <bool E8M0>
-static hipError_t launch_tile(const LinearFp8Args& a, hipStream_t s) { return a.ybf16 ? launch_tile_of<false>(a, s) : launch_tile_of<true>(a, s); }
-
 // How a call is run.
 enum LinearPath { kStreamPath, kSplitPath, kMidPath, kTilePath };
 struct LinearPlan {
@@ -1004,7 +1001,7 @@ hipError_t launch_linear_fp8(LinearFp8Args a, hipStream_t s) {
       return KB <= 48 ? launch_stream<3, 1>(a, s) : launch_stream<4, 1>(a, s);
     case kSplitPath: return launch_split(a, s);
     case kMidPath: return p.rows == 32 ? launch_mid<32>(a, s) : p.rows == 64 ? launch_mid<64>(a, s) : launch_mid<128>(a, s);
-    case kTilePath: return a.e8m0 ? launch_tile<true>(a, s) : launch_tile<false>(a, s);
+    case kTilePath: return a.ybf16 ? launch_tile<false>(a, s) : launch_tile<true>(a, s);
   }
   return hipErrorInvalidValue;
 }

@@ -25,7 +25,8 @@ __device__ __forceinline__ void put_block(const Fp8Out& o, size_t row, int cb, i
 
 // SiLU with the reciprocal instruction (one fp32 step off) in place of a division,
 // whose instructions the gate's kernel would otherwise be bound by; the same
-// infinities, zeros and NaN.
+// infinities and NaN.  Below -87.3, where SiLU is less than 1.2e-36, the reciprocal
+// leaves the normal range and the result may be 0.
 __device__ __forceinline__ float silu_fast(float z) { return z * __builtin_amdgcn_rcpf(1.0f + __expf(-z)); }
 
 // One group of 16 lanes per block of 128 columns of a row.  GATE: the row
@@ -129,7 +130,8 @@ __global__ __launch_bounds__(1024) void k_rmsnorm_fp8(RmsnormFp8Args a) {
     sum = red[0];
     for (int w = 1; w < nw; ++w) sum += red[w];
   }
-  const double r = 1.0 / sqrt(sum / d + (double)a.eps);
+  // (a row whose squares' sum is past fp32 becomes 0, wherever the sum leaves its range)
+  const double r = sum >= 0x1p128 ? 0.0 : 1.0 / sqrt(sum / d + (double)a.eps);
   Fp8Factor m;
   m.hi = (float)r;
   m.lo = m.hi < __builtin_inff() ? (float)(r - m.hi) : 0.f;
@@ -148,18 +150,30 @@ __global__ __launch_bounds__(1024) void k_rmsnorm_fp8(RmsnormFp8Args a) {
 }
 
 namespace {
+// A launch's threads are counted in 32 bits, 16 to a block: larger calls are
+// several launches, of 2^31 elements each (a millisecond of work).
+constexpr uint32_t kLaunchBlocks = 1u << 24;
+
 template <typename T, bool GATE>
-hipError_t rows_launch(const char* name, const void* x, int N, int cols, float t, const Fp8Out& o, hipStream_t s) {
-  const uint32_t blocks = (uint32_t)N * (uint32_t)(o.ld / kFp8Block);
-  const dim3 grid((blocks + 15) / 16);
-  KernelTimer timer(name, s);
-  if (o.e8m0)
-    hipExtLaunchKernelGGL((k_fp8_rows<T, true, GATE>), grid, dim3(256), 0, s, timer.start(), timer.stop(), 0,
-                          static_cast<const T*>(x), cols, t, blocks, o);
-  else
-    hipExtLaunchKernelGGL((k_fp8_rows<T, false, GATE>), grid, dim3(256), 0, s, timer.start(), timer.stop(), 0,
-                          static_cast<const T*>(x), cols, t, blocks, o);
-  return hipGetLastError();
+hipError_t rows_launch(const char* name, const void* x, int N, int cols, float t, const Fp8Out& out, hipStream_t s) {
+  const uint32_t nb = (uint32_t)out.ld / kFp8Block;
+  const int most = (int)(kLaunchBlocks / nb);  // rows of a launch
+  for (int r = 0; r < N; r += most) {
+    const uint32_t blocks = (uint32_t)(N - r < most ? N - r : most) * nb;
+    const dim3 grid((blocks + 15) / 16);
+    const T* xr = static_cast<const T*>(x) + (size_t)r * cols * (GATE ? 2 : 1);
+    Fp8Out o = out;
+    o.q += (size_t)r * o.ld;
+    o.scale = static_cast<uint8_t*>(o.scale) + (size_t)r * nb * (o.e8m0 ? 1 : 4);
+    KernelTimer timer(name, s);
+    if (o.e8m0)
+      hipExtLaunchKernelGGL((k_fp8_rows<T, true, GATE>), grid, dim3(256), 0, s, timer.start(), timer.stop(), 0, xr, cols, t, blocks, o);
+    else
+      hipExtLaunchKernelGGL((k_fp8_rows<T, false, GATE>), grid, dim3(256), 0, s, timer.start(), timer.stop(), 0, xr, cols, t, blocks, o);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 template <typename T>

@@ -96,6 +96,9 @@ def test_linear_arguments():
     assert _linear(y=A) == RANGE and _linear(y=A + G) == RANGE and _linear(y=A + 2 * G + 4096) == RANGE
     assert _linear(y=A + 3 * G) == RANGE and _linear(res=A + 4 * G + 16) == RANGE
     assert _linear(scratch=0) == WORKSPACE and _linear(scratch=A + 5 * G + 64) == ALIGN
+    for scratch in (A, A + G, A + 2 * G + 512, A + 3 * G, A + 4 * G + 256):  # an operand's
+        assert _linear(scratch=scratch) == RANGE
+    assert _linear(res=A + 5 * G) == RANGE
     for N in (1, 60, 400):
         assert _linear(N=N, nbytes=P.raw().cats_linear_fp8_workspace_bytes(N, 256, 256) - 1) == WORKSPACE
 

@@ -71,6 +71,22 @@ def test_quantize_reads_unaligned_rows():
         check_quantised(x, q, s, 1, 0.0)
 
 
+@pytest.mark.parametrize("gate", [False, True])
+def test_rows_of_more_than_one_launch(gate):
+    """More elements than a launch takes (2^31), and than 32 bits address: each row is
+    what a call of few rows makes of it."""
+    cols, N = 8200, 258111 + 9  # 65 blocks a row, 2^24 of them in 258111 rows
+    say("large", gate)
+    x = torch.randn((1024, cols * (1 + gate)), generator=gen(9)).to(torch.bfloat16).to(DEV)
+    call = P.silu_mul_fp8 if gate else P.quantize_fp8
+    x = x.repeat((N + 1023) // 1024, 1)[:N]
+    x[258111:] *= 3
+    q, s = call(x, scale_dtype=E8M0)
+    for lo, hi in ((0, 5), (131000, 131100), (258100, N)):
+        q2, s2 = call(x[lo:hi].contiguous(), scale_dtype=E8M0)
+        assert _same(q[lo:hi], q2) and _same(s[lo:hi], s2)
+
+
 # ---- RMSNorm -------------------------------------------------------------------
 
 # mean of d squares in fp32 with at most 64 + 6 + 16 additions in a chain, half of
@@ -122,6 +138,18 @@ def test_rmsnorm_special_rows():
         assert (qf[3, :40] == 0).all() and (qf[4] == 0).all()
         ok = [0, 1, 5] if eps else [0]
         check_quantised(plain[ok], q[ok], s[ok], 1, NORM_DELTA)
+
+
+@pytest.mark.parametrize("d", [1024, 16384])
+def test_rmsnorm_sum_of_squares_past_fp32(d):
+    """Each lane's squares add up within fp32, the row's do not."""
+    say("rmsnorm overflow", d)
+    x = torch.full((2, d), 6e17)
+    x[1] /= d ** 0.5  # (the squares' sum 3.6e35)
+    q, s = P.rmsnorm_fp8(x.to(DEV))
+    plain = P.rmsnorm(x.to(DEV)).cpu()
+    assert (plain[0] == 0).all() == (6e17 ** 2 * d > torch.finfo(torch.float32).max)
+    check_quantised(plain, q, s, 1, NORM_DELTA)
 
 
 @pytest.mark.parametrize("stype", SCALES, ids=IDS)
