@@ -12,14 +12,40 @@
 namespace cats {
 
 // Stores a lane's eight values (times m) of block (row, cb), A the block's largest
-// finite one, and from the group's first lane its scale.
-template <bool E8M0>
+// finite one, and from the group's first lane its scale.  Where one of the block's
+// values, known to W steps of fp32, may lie on either side of the middle of two
+// e4m3 values (or its largest of an E8M0 scale's limit, or `doubt`), `exact` gives all
+// eight (m included) in 64 bits.  W = 1: fp32 values themselves.
+template <bool E8M0, int W, typename F>
 __device__ __forceinline__ void put_block(const Fp8Out& o, size_t row, int cb, int sub, uint32_t A, const Fp8Factor& m,
-                                          float (&f)[8]) {
+                                          float (&f)[8], bool doubt, const F& exact) {
   Fp8Factor k;
-  const typename Fp8Scale<E8M0>::type s = fp8_scale<E8M0, 8>(A, m, k, f);
-  const uint2 v = {fp8x4(f, k), fp8x4(f + 4, k)};
-  *reinterpret_cast<uint2*>(o.q + row * o.ld + (size_t)cb * kFp8Block + sub * 8) = v;
+  bool plain;
+  typename Fp8Scale<E8M0>::type s = fp8_scale<E8M0, W <= 1, 8>(A, m, k, f, plain);
+  float v[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] = W > 1 ? f[e] * k.hi : times(f[e], k);
+  if constexpr (W == 1) {
+    fix_ties(v, f, A, plain);
+  } else if constexpr (W > 1) {
+    doubt |= near_tie<W>(v);
+    if constexpr (E8M0) doubt |= ((__float_as_uint(times(__uint_as_float(A), m)) + W - 0x600000u) & 0x7fffffu) <= 2 * W;
+    const uint64_t who = __ballot(doubt && plain);
+    if (__builtin_expect(who != 0, 0)) {
+      double x[8], top = 0.0, kx;
+      exact(x);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) top = fabsf(f[e]) < __builtin_inff() ? fmax(top, fabs(x[e])) : top;
+      top = max16(top);
+      // (of the block alone: a row's result does not depend on the rows beside it)
+      if ((who >> (threadIdx.x & 48)) & 0xffffu) {
+        s = Fp8Scale<E8M0>::exact(top, kx);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = fabsf(f[e]) < __builtin_inff() ? to_odd(x[e] * kx) : __builtin_nanf("");
+      }
+    }
+  }
+  *reinterpret_cast<uint2*>(o.q + row * o.ld + (size_t)cb * kFp8Block + sub * 8) = fp8x8(v);
   if (sub == 0) reinterpret_cast<typename Fp8Scale<E8M0>::type*>(o.scale)[row * (o.ld / kFp8Block) + cb] = s;
 }
 
@@ -31,6 +57,8 @@ __device__ __forceinline__ float silu_fast(float z) { return z * __builtin_amdgc
 
 // One group of 16 lanes per block of 128 columns of a row.  GATE: the row
 // holds m gate values, then m up values; h = SiLU(g) u where |SiLU(g)| is not below t.
+// SiLU(z) is within (|z| + 6) 2^-24 of itself, and mostly a quarter of that: a value next
+// to the cutoff is found by 2^-20, a quotient by 14 steps (1.4% of the waves).
 template <typename T, bool E8M0, bool GATE>
 __global__ __launch_bounds__(256) void k_fp8_rows(const T* __restrict__ x, int cols, float t, uint32_t blocks, Fp8Out o) {
   const uint32_t b = blockIdx.x * 16u + threadIdx.x / 16u;
@@ -39,17 +67,29 @@ __global__ __launch_bounds__(256) void k_fp8_rows(const T* __restrict__ x, int c
   const int cb = (int)(b - row * nb), sub = threadIdx.x & 15, c = cb * kFp8Block + sub * 8;
   const T* xr = x + (size_t)row * cols * (GATE ? 2 : 1);
   float f[8];
-  load8(xr, c, cols, f);
+  const Fp8Factor one = {1.f, 0.f};
   if constexpr (GATE) {
-    float u[8];
-    load8(xr + cols, c, cols, u);
+    float u[8], h[8];
+    load8(xr, xr + cols, c, cols, f, u);
+    const float lo = t * (1.f - 0x1p-20f), hi = t * (1.f + 0x1p-20f);  // between them: see `exact`
+    bool off = false;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       const float v = silu_fast(f[e]);
-      f[e] = fabsf(v) < t ? 0.f : v * u[e];
+      off |= (fabsf(v) < lo) != (fabsf(v) < hi);
+      h[e] = fabsf(v) < lo ? 0.f : v * u[e];
     }
+    put_block<E8M0, 14>(o, row, cb, sub, block_max<8>(h), one, h, off, [&](double (&x)[8]) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const double z = f[e], v = z / (1.0 + exp(-z));
+        x[e] = fabs(v) < (double)t ? 0.0 : v * (double)u[e];
+      }
+    });
+  } else {
+    load8(xr, c, cols, f);
+    put_block<E8M0, sizeof(T) == 4 && !E8M0 ? 1 : 0>(o, row, cb, sub, block_max<8>(f), one, f, false, 0);
   }
-  put_block<E8M0>(o, row, cb, sub, block_max<8>(f), Fp8Factor{1.f, 0.f}, f);
 }
 
 // One block of 512 threads per 128 x 128 weights, 32 of them per thread.
@@ -77,12 +117,16 @@ __global__ __launch_bounds__(512) void k_fp8_tiles(const T* __restrict__ x, int 
   __syncthreads();
   a = max16(max(red[sub], red[sub + 16]));
   Fp8Factor k;
-  const typename Fp8Scale<E8M0>::type s = fp8_scale<E8M0, 8 * R>(a, Fp8Factor{1.f, 0.f}, k, &f[0][0]);
+  bool plain;
+  const typename Fp8Scale<E8M0>::type s = fp8_scale<E8M0, true, 8 * R>(a, Fp8Factor{1.f, 0.f}, k, &f[0][0], plain);
 #pragma unroll
   for (int i = 0; i < R; ++i) {
     const int r = r0 + 32 * i;
-    if (r < rows)
-      *reinterpret_cast<uint2*>(o.q + (size_t)r * o.ld + c) = uint2{fp8x4(f[i], k), fp8x4(f[i] + 4, k)};
+    float v[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = times(f[i][e], k);
+    if constexpr (sizeof(T) == 4 && !E8M0) fix_ties(v, f[i], a, plain);
+    if (r < rows) *reinterpret_cast<uint2*>(o.q + (size_t)r * o.ld + c) = fp8x8(v);
   }
   if (threadIdx.x == 0) reinterpret_cast<typename Fp8Scale<E8M0>::type*>(o.scale)[(size_t)rb * nb + cb] = s;
 }
@@ -90,23 +134,37 @@ __global__ __launch_bounds__(512) void k_fp8_tiles(const T* __restrict__ x, int 
 // One block per row, the row in registers (NV chunks of eight columns per thread):
 // one read of x and the residual.
 template <typename T, bool E8M0, int NV>
-__global__ __launch_bounds__(1024) void k_rmsnorm_fp8(RmsnormFp8Args a) {
+__global__ __launch_bounds__(1024, NV == 1 ? 8 : 4) void k_rmsnorm_fp8(RmsnormFp8Args a) {
   __shared__ double red[16];
   const int d = a.d, tid = threadIdx.x, T0 = blockDim.x;
   const size_t row = blockIdx.x;
   const T* xr = static_cast<const T*>(a.x) + row * d;
-  float f[NV][8];
-  float ss = 0.f;
+  // What the additions round off is kept for values next to a middle.  Rows of more than
+  // 8192 columns have no registers for it without fewer waves (2048 rows of 12288: 56 us, 48
+  // without), and no second look.
+  constexpr bool LO = NV == 1;
+  float f[NV][8], lo[LO ? NV : 1][8] = {};
+  double ss = 0.0;
+  if (NV > 1 || !a.residual) {
 #pragma unroll
-  for (int i = 0; i < NV; ++i) load8(xr, (tid + T0 * i) * 8, d, f[i]);
+    for (int i = 0; i < NV; ++i) load8(xr, (tid + T0 * i) * 8, d, f[i]);
+  }
   if (a.residual) {
     float r[NV][8];
+    if constexpr (NV == 1) {
+      load8(xr, a.residual + row * d, tid * 8, d, f[0], r[0]);
+    } else {
 #pragma unroll
-    for (int i = 0; i < NV; ++i) load8(a.residual + row * d, (tid + T0 * i) * 8, d, r[i]);
+      for (int i = 0; i < NV; ++i) load8(a.residual + row * d, (tid + T0 * i) * 8, d, r[i]);
+    }
 #pragma unroll
     for (int i = 0; i < NV; ++i)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) f[i][e] += r[i][e];
+      for (int e = 0; e < 8; ++e) {
+        const float x = f[i][e], sum = x + r[i][e], b = sum - x;
+        if constexpr (LO) lo[i][e] = (x - (sum - b)) + (r[i][e] - b);
+        f[i][e] = sum;
+      }
   }
   if (a.sum) {
 #pragma unroll
@@ -115,14 +173,8 @@ __global__ __launch_bounds__(1024) void k_rmsnorm_fp8(RmsnormFp8Args a) {
 #pragma unroll
   for (int i = 0; i < NV; ++i)
 #pragma unroll
-    for (int e = 0; e < 8; ++e) ss = fmaf(f[i][e], f[i][e], ss);
-  // sums of 16 lanes in fp32 (their roundings average out over the row's many), from
-  // there on in 64 bits
-  ss += dpp_f32<0xb1>(ss);
-  ss += dpp_f32<0x4e>(ss);
-  ss += dpp_f32<0x141>(ss);
-  ss += dpp_f32<0x140>(ss);
-  double sum = ((double)lane_f32(ss, 0) + lane_f32(ss, 16)) + ((double)lane_f32(ss, 32) + lane_f32(ss, 48));
+    for (int e = 0; e < 8; ++e) ss += (double)(f[i][e] * f[i][e]);  // (squares in fp32, whose range they keep)
+  double sum = wave_sum64(ss);
   const int nw = T0 / kWaveSize;
   if (nw > 1) {
     if ((tid & (kWaveSize - 1)) == 0) red[tid / kWaveSize] = sum;
@@ -139,13 +191,20 @@ __global__ __launch_bounds__(1024) void k_rmsnorm_fp8(RmsnormFp8Args a) {
   for (int i = 0; i < NV; ++i) {
     const int c = (tid + T0 * i) * 8;
     if (c >= a.o.ld) continue;
+    float g[8], y[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) y[e] = f[i][e], g[e] = 1.f;
     if (a.gain) {
-      float g[8];
       load8(a.gain, c, d, g);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) f[i][e] *= g[e];
+      for (int e = 0; e < 8; ++e) y[e] *= g[e];
     }
-    put_block<E8M0>(a.o, row, c / kFp8Block, (c / 8) & 15, block_max<8>(f[i]), m, f[i]);
+    // (the sum's and the product's roundings, of the value and of the largest, and the
+    // factor's: 10 steps)
+    put_block<E8M0, LO ? 10 : 0>(a.o, row, c / kFp8Block, (c / 8) & 15, block_max<8>(y), m, y, false, [&](double (&x)[8]) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = ((double)f[i][e] + (double)lo[LO ? i : 0][e]) * (double)g[e] * r;
+    });
   }
 }
 

@@ -5,7 +5,7 @@ import torch
 import paper_2404_08763_amd as P
 from paper_2404_08763_amd import workloads as W
 
-from fp8_util import BLOCK, E8M0, F32, U, check_linear, check_quantised, gen, ld_of, linear_ref, quantised
+from fp8_util import BLOCK, E8M0, F32, U, check_linear, check_quantised, gen, ld_of, linear_ref, quantised, spread
 from gpu_util import kernels_of, say
 
 pytestmark = pytest.mark.gpu
@@ -202,6 +202,47 @@ def test_silu_mul_special_values():
     assert qf[[0, 1, 6, 7]].tolist() == [0, 0, 0, 0]
     assert torch.isnan(qf[[3, 4, 5]]).all()
     assert float(qf[2]) == 448.0 and abs(float(s[0, 0]) * 448.0 - 100.0) < 1e-4
+
+
+@pytest.mark.parametrize("stype", SCALES, ids=IDS)
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["x32", "x16"])
+@pytest.mark.parametrize("op", ["rows", "weights", "norm", "gate"])
+def test_every_value_is_the_nearest(op, dtype, stype):
+    """q against the 64-bit quotients of two million values, none off by fp32's roundings.
+    Left out: quotients within 2^-40 of the middle of two (64 bits do not tell which
+    side a middle is on), and below 2^-6."""
+    say("nearest", op, dtype, stype)
+    N, d = 1001, 2056
+    x = torch.randn((N, d * (1 + (op == "gate"))), generator=gen(11)).to(dtype).to(DEV)
+    if op == "norm":
+        r, g = torch.randn((N, d), generator=gen(12)).to(DEV), (1 + 0.1 * torch.randn(d, generator=gen(13))).to(DEV)
+        q, s = P.rmsnorm_fp8(x, residual=r, gain=g, scale_dtype=stype)
+        v = x.double() + r.double()
+        v = v / (v.square().mean(1, keepdim=True) + 1e-5).sqrt() * g.double()
+    elif op == "gate":
+        q, s = P.silu_mul_fp8(x, t=0.125, scale_dtype=stype)
+        z, u = x.double().split(d, dim=1)
+        v = z / (1 + torch.exp(-z))
+        v = torch.where(v.abs() < 0.125, torch.zeros_like(v), v) * u
+    else:
+        q, s = P.quantize_fp8(x, block_rows=128 if op == "weights" else 1, scale_dtype=stype)
+        v = x.double()
+    up = 128 if op == "weights" else 1
+    v, q, s = v.cpu(), q.cpu()[:, :d].float().double(), s.cpu()
+    if stype == E8M0:
+        quot = v / spread(s, up, N)[:, :d]
+    else:
+        nr, nb = s.shape
+        full = torch.zeros((nr * up, nb * BLOCK), dtype=torch.float64)
+        full[:N, :d] = v
+        top = full.abs().view(nr, up, nb, BLOCK).amax(dim=(1, 3))
+        quot = v * 448.0 / top.repeat_interleave(up, 0)[:N].repeat_interleave(BLOCK, 1)[:, :d]
+    step = 2.0 ** (torch.frexp(quot)[1].double() - 4)
+    steps = quot / step
+    clear = (quot.abs() >= 2.0 ** -6) & (((steps - steps.floor()) - 0.5).abs() > 2.0 ** -40)
+    assert clear.double().mean() > 0.4  # (the cutoff leaves a half)
+    wrong = clear & (q != torch.round(steps) * step)
+    assert not wrong.any(), int(wrong.sum())
 
 
 # ---- linear --------------------------------------------------------------------------
