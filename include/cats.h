@@ -349,10 +349,11 @@ cats_status cats_rmsnorm(const float* x, float* xn, int32_t B, int32_t d, float 
  * The calls that write such matrices take, with a the block's largest finite
  * magnitude, the scale a / 448 in fp32 (2^-126 if that is less), or the
  * smallest 2^e with a <= 448 * 2^e and e >= -126, and 1 where a is 0; q is the
- * e4m3 value nearest to the element times 448 / a or 2^-e (ties to even), as 64 bits
- * give them; fp32's roundings may take the other of two about equally near ones
- * where q is below 2^-6 or the scale 2^-126, and for RMSNorm of more than 8192 columns.  An infinite or NaN element becomes e4m3's NaN;
- * the block's other elements are what they are without it.
+ * e4m3 value nearest to the element times 448 / a or 2^-e (ties to even), as 64
+ * bits give them; fp32's roundings may take the other of two about equally near
+ * ones where q is below 2^-6 or the scale 2^-126, and for RMSNorm of more than
+ * 8192 columns.  An infinite or NaN element becomes e4m3's NaN; the block's other
+ * elements are what they are without it.
  * All four calls are enqueue only and may be captured in a graph. */
 #define CATS_FP8_BLOCK 128
 typedef enum { CATS_SCALE_F32 = 0, CATS_SCALE_E8M0 = 1 } cats_scale_type;
@@ -380,7 +381,8 @@ cats_status cats_quantize_fp8(const void* x, int32_t dtype, int32_t rows, int32_
  *   gain      dev [d] fp32; NULL: 1 (as cats_rmsnorm)
  *   sum_out   dev [N x d] fp32, receives s; NULL: not written.  May be the
  *             residual itself, or x if that is fp32.
- * The sum and the row are fp32 or more until q, the mean 64 bits.  Rows whose sum of squares overflows fp32 become 0, as cats_rmsnorm's.
+ * The sum and the row are fp32 or more until q, the mean 64 bits.  Rows whose
+ * sum of squares overflows fp32 become 0, as cats_rmsnorm's.
  * 1 <= N <= CATS_MAX_FP8_ROWS, 1 <= d <= CATS_MAX_FP8_COLS, eps >= 0. */
 cats_status cats_rmsnorm_fp8(const void* x, int32_t dtype, const float* residual, const float* gain, int32_t N,
                              int32_t d, float eps, int32_t stype, float* sum_out, void* q, void* scale, void* stream);

@@ -409,7 +409,7 @@ constexpr int kTileGroup = 6;  // (whole columns: 5% slower for 2048 rows 4096 -
 // (fp32 scales 226 us, 2.1), where the library's product of one scale for all takes 153.
 // EXACT, fp32 outputs: 256 x 128, the bf16 instructions; operands are widened in the
 // reading phase, under the other group's products (in the multiplying phase:
-// 410 us).  The same size 382 us, 1.26 PFLOP/s; the library's bf16 product, whose
+// 410 us).  The same size 371 to 412 us by the card, 1.17 to 1.30 PFLOP/s; the library's bf16 product, whose
 // operands have twice the bytes, takes 305.  Tiles of 32 x 32 had the same time or more.
 template <bool EXACT> struct TileGeom;
 template <> struct TileGeom<false> {
