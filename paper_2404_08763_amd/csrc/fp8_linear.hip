@@ -14,6 +14,8 @@
 // bound the call (k_fp8_tile of bf16 outputs).  Elsewhere the values are widened
 // to bf16, which holds them exactly, on their way from the registers to the bf16
 // instructions, whose sums are exact to fp32.
+#include <algorithm>
+
 #include "fp8.hpp"
 #include "internal.hpp"
 #include "stream.hpp"
@@ -730,10 +732,10 @@ static hipError_t launch_tile(const LinearFp8Args& a, hipStream_t s) {
 // parts of the column blocks; parts meet in k_fp8_join.  Values are widened
 // between LDS and the bf16 instructions for every output type.  A step's operands
 // go from memory straight to LDS while the step before is multiplied, one barrier
-// a step.  Bound by a step's chain of reads, widening and products (1.2 us of a
-// lone block of 128 x 128, 1.0 each of two on a compute unit) where there are few
-// steps, by the parts' traffic and the second launch where there are many parts:
-// 256 rows 4096 -> 4096 22 us, 101 rows 7001 -> 2857 17.5.
+// a step.  Bound by a step's chain of reads, widening and products (0.9, 1.0 and 1.2 us of
+// a lone block of 32, 64 and 128 rows, 0.5, 0.6 and 1.0 each of several on a compute unit),
+// by the parts' traffic and the second launch where there are many parts: 300 rows
+// 4096 -> 4096 24 us, 101 rows 7001 -> 2857 18, 312 rows 256 -> 3106 6.7.
 template <int TN> struct MidGeom;
 template <> struct MidGeom<128> { static constexpr int WN = 2, MI = 2, NB = 2; };  // waves along x's rows, 32 x 32 tiles of a wave
 template <> struct MidGeom<64> { static constexpr int WN = 2, MI = 2, NB = 1; };
@@ -939,41 +941,56 @@ struct LinearPlan {
   int S;     // parts of the reduction
 };
 
-// us of a column block's step, from the sizes below over their steps: of a round of
-// 256 tiles (one a compute unit) of the two-group kernel, and of the 128 x 128 kernel, whose
-// blocks of one compute unit overlap.
-constexpr int kTileStepF32 = 172, kTileStepE8m0 = 160, kTileStep = 210;  // in 1/100: fp32 outputs, bf16 by type of scale
-constexpr int kMidStepOne = 127, kMidStepEach = 103;
+// What a column block's step takes, in 1/100 us, measured on 112 steps with the weights
+// from memory: of a round of 256 tiles (one a compute unit) of the two-group kernel by
+// output and type of scale; of k_fp8_mid's blocks of 32, 64 and 128 rows, one on a compute
+// unit and each of several, and what larger tiles take longer to start and end.
+constexpr int kTileStepF32 = 172, kTileStepE8m0 = 160, kTileStep = 210;
+constexpr int kMidParts[] = {1, 2, 3, 4, 5, 6, 8, 12, 16, 24};
+constexpr int kMidStepOne[3] = {95, 97, 123}, kMidStepEach[3] = {46, 62, 99}, kMidStart[3] = {0, 40, 100};
+// The second launch; bytes of the parts' sums, written and read, and of weights, which two
+// blocks that run beside each other both fetch, in 1/100 us.
+constexpr int kJoin = 400, kJoinBytes = 40000, kFetchBytes = 55000;
 
-// us a call, weights rotated so that they come from memory:
 // Up to 16 rows, and up to 32 of no more than 32 column blocks: the streaming kernel
-// (32 rows 4096 -> 22016 22 against 26 of the 128 x 32 tiles; 1 row 8192 -> 28672 46, split
+// (32 rows 4096 -> 22016 22 us against 26 of the 128 x 32 tiles; 1 row 8192 -> 28672 46, split
 // 50), unless a wave had more than four column blocks of x to keep.
-// Above: 128 outputs x 32, 64 or 128 rows, in parts while there are fewer blocks than
-// compute units take (256, or 384 of the small tiles, of which three fit one), but of
-// six column blocks at least (101 rows 7001 -> 2857, fp32: 4 / 8 / 16 parts 20 / 18 / 21;
-// 256 rows 4096 -> 4096: 2 / 4 / 8 / 12 parts 27 / 22 / 26 / 31; 64 rows 11008 -> 4096: 4 / 8 /
-// 16 / 20 parts 29 / 21 / 22 / 26; 32 rows 4096 -> 22016, 172 tiles: 1 / 2 / 3 parts 35 / 26 / 29).
-// The two-group kernel, with its larger tiles, once they fill the compute units
-// better (two-group / 128 x 128: 512 rows 4096 -> 22016, bf16 71 / 102, fp32 111 / 104; 256
-// rows, bf16 with fp32 scales 70 / 62, with E8M0 52 / 62; 2048 rows 4096 -> 4096, fp32 60 / 74;
-// 1024 rows 11008 -> 4096, fp32 128 / 102; 4096 rows 512 -> 4096, bf16 21 / 34).
+// Above: what takes least by the steps and rounds of its blocks, of 128 outputs x 32, 64
+// or 128 rows in S parts and of the two-group kernel, whose larger tiles need a filled
+// chip (us, weights from memory; 128 rows from 65 on, in parts of six column blocks and more,
+// and this rule: 304 rows 3240 -> 286 14.4 / 10.3; 96 rows 1128 -> 3304 14.0 / 8.5; 312 rows
+// 256 -> 3106 10.4 / 6.7; 300 rows 4096 -> 4096 29.5 / 24.1; 200 rows 14336 -> 512 18.0 / 15.2;
+// 1743 rows 9346 -> 852 51.8 / 54.3.  Two-group / 128 x 128: 512
+// rows 4096 -> 22016, bf16 71 / 102, fp32 111 / 104; 256 rows, bf16 with fp32 scales 70 / 62,
+// with E8M0 52 / 62; 2048 rows 4096 -> 4096, fp32 60 / 74; 1024 rows 11008 -> 4096, fp32
+// 128 / 102; 4096 rows 512 -> 4096, bf16 21 / 34).
 static LinearPlan linear_plan(int N, int n, int KB, bool bf16, bool e8m0) {
   const int each = (KB + kStreamWaves - 1) / kStreamWaves;  // column blocks of a wave
   if (N <= 16) return {each <= 4 ? kStreamPath : kSplitPath, 16, 1};
   if (N <= 32 && each <= 2) return {kStreamPath, 32, 1};
-  const int rows = N <= 32 ? 32 : N <= 64 ? 64 : 128;
-  const int64_t blocks = (int64_t)((n + 127) / 128) * ((N + rows - 1) / rows);
-  const int64_t rounds = (blocks + 255) / 256;
-  if (rows == 128) {
-    const int wide = bf16 ? 256 : 128;
-    const int64_t tiles = (int64_t)((n + 255) / 256) * ((N + wide - 1) / wide);
-    const int step = !bf16 ? kTileStepF32 : e8m0 ? kTileStepE8m0 : kTileStep;
-    if (step * ((tiles + 255) / 256) < (rounds == 1 ? kMidStepOne : kMidStepEach * rounds)) return {kTilePath, wide, 1};
+  LinearPlan best = {kMidPath, 0, 1};
+  int64_t least = INT64_MAX;
+  const int64_t columns = (n + 127) / 128;
+  for (int i = 0; i < 3; ++i) {
+    const int rows = 32 << i;
+    if (i > 0 && rows >= 2 * N) break;
+    const int64_t high = (N + rows - 1) / rows, blocks = columns * high;
+    const int64_t fetch = columns * KB * (128 * 128) * (high > 1 ? 2 : 1);
+    for (const int S : kMidParts) {
+      if (S > 1 && (2 * S > KB || blocks * S > 768)) break;  // (three a compute unit)
+      const int64_t all = blocks * S, rounds = (all + 255) / 256;
+      // (a last round that fills part of the chip goes with less traffic beside it)
+      const int64_t step = std::max<int64_t>(kMidStepOne[i], kMidStepEach[i] * (3 * 256 * rounds + all) / 1024);
+      const int64_t steps = std::max((KB + S - 1) / S * step, fetch / kFetchBytes);
+      const int64_t us = kMidStart[i] + steps + (S > 1 ? kJoin + (int64_t)S * N * n * 8 / kJoinBytes : 0);
+      if (us < least) least = us, best.rows = rows, best.S = S;
+    }
   }
-  const int64_t S = rows == 128 ? (256 + blocks / 2) / blocks : 384 / blocks;
-  const int most = KB / 6 > 1 ? KB / 6 : 1;
-  return {kMidPath, rows, (int)(S < 1 ? 1 : S > most ? most : S)};
+  const int wide = bf16 ? 256 : 128;
+  const int64_t tiles = (int64_t)((n + 255) / 256) * ((N + wide - 1) / wide);
+  const int step = !bf16 ? kTileStepF32 : e8m0 ? kTileStepE8m0 : kTileStep;
+  if (N > 64 && KB * step * ((tiles + 255) / 256) < least) return {kTilePath, wide, 1};
+  return best;
 }
 
 static int partial_pitch(int n) { return (n + 3) / 4 * 4; }

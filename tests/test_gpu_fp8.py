@@ -257,7 +257,7 @@ LINEAR = [(1, 1, 1), (1, 16, 128), (1, 6144, 4096), (2, 130, 129), (5, 40, 7001)
           (33, 257, 384), (48, 1000, 3000), (64, 512, 2048), (65, 4096, 640), (100, 300, 2000), (128, 513, 1152),
           (129, 4097, 128), (255, 640, 4096), (257, 1000, 4224), (300, 2048, 8320), (512, 1024, 256), (700, 3001, 1000),
           (1024, 2048, 384), (2000, 4100, 300), (1537, 4097, 1153), (1537, 4100, 128), (1540, 4100, 200), (1537, 4097, 300),
-          (1537, 4100, 640), (8, 300, 9000), (16, 100, 8192), (20, 515, 5000), (32, 4097, 4096)]
+          (1537, 4100, 640), (8, 300, 9000), (16, 100, 8192), (20, 515, 5000), (32, 4097, 4096), (37, 11413, 1668), (1743, 852, 9346)]
 
 
 @pytest.mark.parametrize("stype", SCALES, ids=IDS)
@@ -293,6 +293,8 @@ def test_linear(N, n, k, stype):
     (100, 300, 2000, torch.bfloat16, F32, {"linear_fp8_mid", "linear_fp8_join"}),
     (1024, 2048, 384, torch.float32, F32, {"linear_fp8_mid"}),
     (700, 3001, 1000, torch.float32, F32, {"linear_fp8_mid"}),
+    (300, 2048, 8320, torch.float32, F32, {"linear_fp8_mid", "linear_fp8_join"}),
+    (1743, 852, 9346, torch.bfloat16, E8M0, {"linear_fp8_mid", "linear_fp8_join"}),
     (1537, 4097, 1153, torch.float32, F32, {"linear_fp8_tile_f32"}),
     (1537, 4097, 1153, torch.float32, E8M0, {"linear_fp8_tile_f32"}),
     (2000, 4100, 300, torch.bfloat16, F32, {"linear_fp8_tile"}),
