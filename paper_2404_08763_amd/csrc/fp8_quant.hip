@@ -16,11 +16,11 @@ namespace cats {
 // Stores a lane's eight values (times m) of block (row, cb), A the block's largest
 // finite one, and from the group's first lane its scale.  Where one of the block's
 // values, known to W steps of fp32, may lie on either side of the middle of two
-// e4m3 values (or its largest of an E8M0 scale's limit, or `doubt`), `exact` gives all
+// e4m3 values (or its largest of an E8M0 scale's limit), `exact` gives all
 // eight (m included) in 64 bits.  W = 1: fp32 values themselves.
 template <bool E8M0, int W, typename F>
 __device__ __forceinline__ void put_block(const Fp8Out& o, size_t row, int cb, int sub, uint32_t A, const Fp8Factor& m,
-                                          float (&f)[8], bool doubt, const F& exact) {
+                                          float (&f)[8], const F& exact) {
   Fp8Factor k;
   bool plain;
   typename Fp8Scale<E8M0>::type s = fp8_scale<E8M0, W <= 1, 8>(A, m, k, f, plain);
@@ -30,7 +30,7 @@ __device__ __forceinline__ void put_block(const Fp8Out& o, size_t row, int cb, i
   if constexpr (W == 1) {
     fix_ties(v, f, A, plain);
   } else if constexpr (W > 1) {
-    doubt |= near_tie<W>(v);
+    bool doubt = near_tie<W>(v);
     if constexpr (E8M0) doubt |= ((__float_as_uint(times(__uint_as_float(A), m)) + W - 0x600000u) & 0x7fffffu) <= 2 * W;
     const uint64_t who = __ballot(doubt && plain);
     if (__builtin_expect(who != 0, 0)) {
@@ -73,7 +73,7 @@ __global__ __launch_bounds__(256) void k_fp8_rows(const T* __restrict__ x, int c
   if constexpr (GATE) {
     float u[8], h[8];
     load8(xr, xr + cols, c, cols, f, u);
-    const float lo = t * (1.f - 0x1p-20f), hi = t * (1.f + 0x1p-20f);  // between them: see `exact`
+    const float lo = t * (1.f - 0x1p-20f), hi = t * (1.f + 0x1p-20f);  // between them: 64 bits decide
     bool off = false;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
@@ -81,7 +81,14 @@ __global__ __launch_bounds__(256) void k_fp8_rows(const T* __restrict__ x, int c
       off |= (fabsf(v) < lo) != (fabsf(v) < hi);
       h[e] = fabsf(v) < lo ? 0.f : v * u[e];
     }
-    put_block<E8M0, 14>(o, row, cb, sub, block_max<8>(h), one, h, off, [&](double (&x)[8]) {
+    if (__builtin_expect(__any(off), 0)) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const double z = f[e];
+        if (fabs(z / (1.0 + exp(-z))) < (double)t) h[e] = 0.f;
+      }
+    }
+    put_block<E8M0, 14>(o, row, cb, sub, block_max<8>(h), one, h, [&](double (&x)[8]) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const double z = f[e], v = z / (1.0 + exp(-z));
@@ -90,7 +97,7 @@ __global__ __launch_bounds__(256) void k_fp8_rows(const T* __restrict__ x, int c
     });
   } else {
     load8(xr, c, cols, f);
-    put_block<E8M0, sizeof(T) == 4 && !E8M0 ? 1 : 0>(o, row, cb, sub, block_max<8>(f), one, f, false, 0);
+    put_block<E8M0, sizeof(T) == 4 && !E8M0 ? 1 : 0>(o, row, cb, sub, block_max<8>(f), one, f, 0);
   }
 }
 
@@ -205,7 +212,7 @@ __global__ __launch_bounds__(1024, NV == 1 ? 8 : 4) void k_rmsnorm_fp8(RmsnormFp
     }
     // (the sum's and the product's roundings, of the value and of the largest, and the
     // factor's: 10 steps)
-    put_block<E8M0, LO ? 10 : 0>(a.o, row, c / kFp8Block, (c / 8) & 15, block_max<8>(y), m, y, false, [&](double (&x)[8]) {
+    put_block<E8M0, LO ? 10 : 0>(a.o, row, c / kFp8Block, (c / 8) & 15, block_max<8>(y), m, y, [&](double (&x)[8]) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) x[e] = ((double)f[i][e] + (double)lo[LO ? i : 0][e]) * (double)g[e] * r;
     });
