@@ -131,11 +131,11 @@ __device__ __forceinline__ uint2 fp8x8(const float (&v)[8]) {
 // Such values, one in 2^19 / W, are looked at again in 64 bits, so that q is the
 // nearest value and not one of the two nearest.  (Below 2^-6, e4m3's
 // subnormals, of which fp32 has 2^14 steps to one and more, values are left as they are.)
-template <int W> __device__ __forceinline__ bool near_tie(const float (&v)[8]) {
+__device__ __forceinline__ bool near_tie(const float (&v)[8], uint32_t W) {
   uint32_t a = ~0u;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) a = min(a, (__float_as_uint(v[e]) << 12) + (0x80000000u + ((uint32_t)W << 12)));
-  return a < ((uint32_t)(2 * W) << 12);
+  for (int e = 0; e < 8; ++e) a = min(a, (__float_as_uint(v[e]) << 12) + (0x80000000u + (W << 12)));
+  return a < (2u * W << 12);
 }
 // v, rounded from a number `above` or `below` it, rounded to odd instead: on the side
 // of any middle that the number is on.
@@ -152,7 +152,7 @@ __device__ __forceinline__ float to_odd(double x) {
 // Quantisation of fp32 alone: v = f 448 / A to one rounding, and f 448 beside v A is
 // exact in 64 bits.  (Of bf16 no f 448 / A lies next to a middle but on it.)
 __device__ __forceinline__ void fix_ties(float (&v)[8], const float (&f)[8], uint32_t A, bool plain) {
-  if (__builtin_expect(__any(plain && near_tie<1>(v)), 0)) {
+  if (__builtin_expect(__any(plain && near_tie(v, 1)), 0)) {
     const double a = __uint_as_float(A);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {

@@ -14,24 +14,26 @@
 namespace cats {
 
 // Stores a lane's eight values (times m) of block (row, cb), A the block's largest
-// finite one, and from the group's first lane its scale.  Where one of the block's
-// values, known to W steps of fp32, may lie on either side of the middle of two
-// e4m3 values (or its largest of an E8M0 scale's limit), `exact` gives all
-// eight (m included) in 64 bits.  W = 1: fp32 values themselves.
-template <bool E8M0, int W, typename F>
+// finite one, and from the group's first lane its scale.
+//   kAgain: where one of the block's values, known to `steps` of fp32, may lie on either
+//     side of the middle of two e4m3 values (or its largest of an E8M0 scale's limit),
+//     `exact` gives all eight (m included) in 64 bits;
+//   kFp32: the values are fp32 numbers and m is 1;  kAsIs: no second look.
+enum Fp8Look { kAsIs, kFp32, kAgain };
+template <bool E8M0, Fp8Look LOOK, typename F>
 __device__ __forceinline__ void put_block(const Fp8Out& o, size_t row, int cb, int sub, uint32_t A, const Fp8Factor& m,
-                                          float (&f)[8], const F& exact) {
+                                          float (&f)[8], uint32_t steps, const F& exact) {
   Fp8Factor k;
   bool plain;
-  typename Fp8Scale<E8M0>::type s = fp8_scale<E8M0, W <= 1, 8>(A, m, k, f, plain);
+  typename Fp8Scale<E8M0>::type s = fp8_scale<E8M0, LOOK != kAgain, 8>(A, m, k, f, plain);
   float v[8];
 #pragma unroll
-  for (int e = 0; e < 8; ++e) v[e] = W > 1 ? f[e] * k.hi : times(f[e], k);
-  if constexpr (W == 1) {
+  for (int e = 0; e < 8; ++e) v[e] = LOOK == kAgain ? f[e] * k.hi : times(f[e], k);
+  if constexpr (LOOK == kFp32) {
     fix_ties(v, f, A, plain);
-  } else if constexpr (W > 1) {
-    bool doubt = near_tie<W>(v);
-    if constexpr (E8M0) doubt |= ((__float_as_uint(times(__uint_as_float(A), m)) + W - 0x600000u) & 0x7fffffu) <= 2 * W;
+  } else if constexpr (LOOK == kAgain) {
+    bool doubt = near_tie(v, steps);
+    if constexpr (E8M0) doubt |= ((__float_as_uint(times(__uint_as_float(A), m)) + steps - 0x600000u) & 0x7fffffu) <= 2u * steps;
     const uint64_t who = __ballot(doubt && plain);
     if (__builtin_expect(who != 0, 0)) {
       double x[8], top = 0.0, kx;
@@ -55,12 +57,22 @@ __device__ __forceinline__ void put_block(const Fp8Out& o, size_t row, int cb, i
 // whose instructions the gate's kernel would otherwise be bound by; the same
 // infinities and NaN.  Below -87.3, where SiLU is less than 1.2e-36, the reciprocal
 // leaves the normal range and the result may be 0.
-__device__ __forceinline__ float silu_fast(float z) { return z * __builtin_amdgcn_rcpf(1.0f + __expf(-z)); }
+// e^-z with what its argument rounds off (-z log2 e = a + r): within 4.4 2^-24 of
+// SiLU, measured over every z.  Without it 10 2^-24 at z = -10, 30 from -22 on and 65 at -87: no
+// few steps find the values next to a middle or the cutoff then (2048 x 14336 bf16 28.5
+// us, with it 29.8).
+__device__ __forceinline__ float silu_fast(float z) {
+  constexpr float L = 0x1.715476p+0f, LLO = 0x1.4ae0cp-26f, LN2 = 0x1.62e43p-1f;  // log2 e = L + LLO
+  const float c = __builtin_amdgcn_fmed3f(z, -3e38f, 100.f);  // (past 100 e^-z counts for nothing)
+  const float a = c * -L, r = fmaf(c, -LLO, fmaf(c, -L, -a));
+  return z * __builtin_amdgcn_rcpf(fmaf(__builtin_amdgcn_exp2f(a), fmaf(r, LN2, 1.f), 1.f));
+}
 
 // One group of 16 lanes per block of 128 columns of a row.  GATE: the row
 // holds m gate values, then m up values; h = SiLU(g) u where |SiLU(g)| is not below t.
-// SiLU(z) is within (|z| + 6) 2^-24 of itself, and mostly a quarter of that: a value next
-// to the cutoff is found by 2^-20, a quotient by 14 steps (1.4% of the waves).
+// A value next to the cutoff is found by 2^-21.  A product is off by SiLU's error and its own
+// rounding, with fp32 scales the quotient by the largest's too and by four half steps
+// of the factor and its use: 6 and 15 (0.6 and 1.5% of the waves).
 template <typename T, bool E8M0, bool GATE>
 __global__ __launch_bounds__(256) void k_fp8_rows(const T* __restrict__ x, int cols, float t, uint32_t blocks, Fp8Out o) {
   const uint32_t b = blockIdx.x * 16u + threadIdx.x / 16u;
@@ -73,7 +85,7 @@ __global__ __launch_bounds__(256) void k_fp8_rows(const T* __restrict__ x, int c
   if constexpr (GATE) {
     float u[8], h[8];
     load8(xr, xr + cols, c, cols, f, u);
-    const float lo = t * (1.f - 0x1p-20f), hi = t * (1.f + 0x1p-20f);  // between them: 64 bits decide
+    const float lo = t * (1.f - 0x1p-21f), hi = t * (1.f + 0x1p-21f);  // between them: 64 bits decide
     bool off = false;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
@@ -88,7 +100,7 @@ __global__ __launch_bounds__(256) void k_fp8_rows(const T* __restrict__ x, int c
         if (fabs(z / (1.0 + exp(-z))) < (double)t) h[e] = 0.f;
       }
     }
-    put_block<E8M0, 14>(o, row, cb, sub, block_max<8>(h), one, h, [&](double (&x)[8]) {
+    put_block<E8M0, kAgain>(o, row, cb, sub, block_max<8>(h), one, h, E8M0 ? 6 : 15, [&](double (&x)[8]) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const double z = f[e], v = z / (1.0 + exp(-z));
@@ -97,7 +109,7 @@ __global__ __launch_bounds__(256) void k_fp8_rows(const T* __restrict__ x, int c
     });
   } else {
     load8(xr, c, cols, f);
-    put_block<E8M0, sizeof(T) == 4 && !E8M0 ? 1 : 0>(o, row, cb, sub, block_max<8>(f), one, f, 0);
+    put_block<E8M0, sizeof(T) == 4 && !E8M0 ? kFp32 : kAsIs>(o, row, cb, sub, block_max<8>(f), one, f, 0, 0);
   }
 }
 
@@ -212,7 +224,7 @@ __global__ __launch_bounds__(1024, NV == 1 ? 8 : 4) void k_rmsnorm_fp8(RmsnormFp
     }
     // (the sum's and the product's roundings, of the value and of the largest, and the
     // factor's: 10 steps)
-    put_block<E8M0, LO ? 10 : 0>(a.o, row, c / kFp8Block, (c / 8) & 15, block_max<8>(y), m, y, [&](double (&x)[8]) {
+    put_block<E8M0, LO ? kAgain : kAsIs>(a.o, row, c / kFp8Block, (c / 8) & 15, block_max<8>(y), m, y, 10, [&](double (&x)[8]) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) x[e] = ((double)f[i][e] + (double)lo[LO ? i : 0][e]) * (double)g[e] * r;
     });
