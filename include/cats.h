@@ -382,7 +382,9 @@ cats_status cats_quantize_fp8(const void* x, int32_t dtype, int32_t rows, int32_
  *   sum_out   dev [N x d] fp32, receives s; NULL: not written.  May be the
  *             residual itself, or x if that is fp32.
  * The sum and the row are fp32 or more until q, the mean 64 bits.  Rows whose
- * sum of squares overflows fp32 become 0, as cats_rmsnorm's.
+ * sum of squares overflows fp32 become 0, as cats_rmsnorm's, and one below
+ * fp32's least number counts as 0 (with eps = 0 such a row is NaN).  s times gain is an fp32
+ * number: past its range it is infinite.
  * 1 <= N <= CATS_MAX_FP8_ROWS, 1 <= d <= CATS_MAX_FP8_COLS, eps >= 0. */
 cats_status cats_rmsnorm_fp8(const void* x, int32_t dtype, const float* residual, const float* gain, int32_t N,
                              int32_t d, float eps, int32_t stype, float* sum_out, void* q, void* scale, void* stream);

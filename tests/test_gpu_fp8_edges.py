@@ -97,3 +97,45 @@ def test_gate_values_far_below_zero_are_the_nearest(stype):
     wrong = clear & (q.cpu().float().double() != want)
     assert clear.double().mean() > 0.9
     assert not wrong.any(), int(wrong.sum())
+
+
+@pytest.mark.parametrize("res", [False, True])
+def test_norm_values_next_to_a_middle_are_the_nearest(res):
+    """Rows of two, f0 and f1 with sqrt(2) f1 / |f| next to (2 j + 1) / 16: which side of the
+    middle q = 256 times that falls goes by the squares' roundings, and by what the residual's
+    addition rounds off."""
+    say("norm next to a middle", res)
+    N = 1 << 16
+    f0 = (1 + torch.rand(N, generator=gen(31))).double()
+    T = (8.5 + torch.randint(0, 8, (N,), generator=gen(32)).double()) / 16
+    x = torch.stack([f0.float(), (f0 * T / torch.sqrt(2 - T * T)).float()], 1)
+    r = x * (2.0 ** -25 * (2 * torch.rand((N, 2), generator=gen(33)) - 1)) if res else None
+    q, s = P.rmsnorm_fp8(x.to(DEV), residual=r.to(DEV) if res else None, eps=0.0, scale_dtype=E8M0)
+    assert (s.float() == 2.0 ** -8).all()
+    f = x.double() + (r.double() if res else 0.0)
+    quot = f / torch.sqrt(f.square().mean(dim=1, keepdim=True)) * 256.0
+    want, clear = _nearest(quot)
+    wrong = clear & (q.cpu()[:, :2].float().double() != want)
+    assert clear.double().mean() > 0.9
+    assert not wrong.any(), int(wrong.sum())
+
+
+@pytest.mark.parametrize("stype", SCALES, ids=IDS)
+def test_norm_of_infinite_sums(stype):
+    """An infinity in x or the residual, or an addition past fp32, makes NaN of its element and
+    zeros of the row's others; the rows beside are what they are without it."""
+    say("norm infinite sums", stype)
+    x, r = torch.randn((5, 300), generator=gen(41)), torch.randn((5, 300), generator=gen(42))
+    want = P.rmsnorm_fp8(x.to(DEV), residual=r.to(DEV), scale_dtype=stype)
+    x[1, 7] = float("inf")
+    r[2, 150] = -float("inf")
+    x[3, 299] = r[3, 299] = 3e38
+    q, s = P.rmsnorm_fp8(x.to(DEV), residual=r.to(DEV), scale_dtype=stype)
+    qf = q.float().cpu()[:, :300]
+    for row, c in ((1, 7), (2, 150), (3, 299)):
+        bad = torch.zeros(300, dtype=torch.bool)
+        bad[c] = True
+        assert torch.equal(torch.isnan(qf[row]), bad) and (qf[row][~bad] == 0).all()
+    for row in (0, 4):
+        assert torch.equal(q[row].view(torch.uint8), want[0][row].view(torch.uint8))
+        assert torch.equal(s[row].view(torch.uint8), want[1][row].view(torch.uint8))
