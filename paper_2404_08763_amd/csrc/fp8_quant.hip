@@ -18,7 +18,8 @@ namespace cats {
 //   kAgain: where one of the block's values, known to `steps` of fp32, may lie on either
 //     side of the middle of two e4m3 values (or its largest of an E8M0 scale's limit),
 //     `exact` gives all eight (m included) in 64 bits;
-//   kFp32: the values are fp32 numbers and m is 1;  kAsIs: no second look.
+//   kFp32: the values are fp32 numbers and m, with fp32 scales, counts for the scale alone;
+//   kAsIs: no second look.
 enum Fp8Look { kAsIs, kFp32, kAgain };
 template <bool E8M0, Fp8Look LOOK, typename F>
 __device__ __forceinline__ void put_block(const Fp8Out& o, size_t row, int cb, int sub, uint32_t A, const Fp8Factor& m,
@@ -156,7 +157,11 @@ __global__ __launch_bounds__(512) void k_fp8_tiles(const T* __restrict__ x, int 
 // One block per row, the row in registers (NV chunks of eight columns per thread):
 // one read of x and the residual, all under way together.  One row of 4096 takes 2.8 us:
 // the loads, the sum over the block and the second reduction of its blocks' largest.
-template <typename T, bool E8M0, int NV>
+// BARE: x alone, without residual and gain, and fp32 scales.  Its quotients are
+// quantisation's, f 448 / A, of which bf16 numbers often lie on the middle of two values and
+// never next to it: 4096 x 4096 bf16 16.2 us, 29.1 with the others' second look, which two waves
+// of three took.
+template <typename T, bool E8M0, int NV, bool BARE>
 __global__ __launch_bounds__(1024, NV == 1 ? 8 : 4) void k_rmsnorm_fp8(RmsnormFp8Args a) {
   __shared__ double red[16];
   const int d = a.d, tid = threadIdx.x, T0 = blockDim.x;
@@ -165,22 +170,23 @@ __global__ __launch_bounds__(1024, NV == 1 ? 8 : 4) void k_rmsnorm_fp8(RmsnormFp
   // What the additions round off is kept for values next to a middle.  Rows of more than
   // 8192 columns have no registers for it without fewer waves (2048 rows of 12288: 56 us, 48
   // without), and no second look.
-  constexpr bool LO = NV == 1;
+  constexpr bool LO = NV == 1 && !BARE;
   float f[NV][8], lo[LO ? NV : 1][8] = {};
   // The row's factor reaches q with E8M0 scales alone: there the squares are those of 64
-  // bits (4096 x 4096 bf16 17.3 -> 18.0 us).
+  // bits (4096 x 4096 bf16 17.3 -> 18.2 us).
   double ss = 0.0;
-  if (NV > 1 || !a.residual) {
+  const float *residual = BARE ? nullptr : a.residual, *gain = BARE ? nullptr : a.gain;
+  if (NV > 1 || !residual) {
 #pragma unroll
     for (int i = 0; i < NV; ++i) load8(xr, (tid + T0 * i) * 8, d, f[i]);
   }
-  if (a.residual) {
+  if (residual) {
     float r[NV][8];
     if constexpr (NV == 1) {
-      load8(xr, a.residual + row * d, tid * 8, d, f[0], r[0]);
+      load8(xr, residual + row * d, tid * 8, d, f[0], r[0]);
     } else {
 #pragma unroll
-      for (int i = 0; i < NV; ++i) load8(a.residual + row * d, (tid + T0 * i) * 8, d, r[i]);
+      for (int i = 0; i < NV; ++i) load8(residual + row * d, (tid + T0 * i) * 8, d, r[i]);
     }
 #pragma unroll
     for (int i = 0; i < NV; ++i)
@@ -227,14 +233,15 @@ __global__ __launch_bounds__(1024, NV == 1 ? 8 : 4) void k_rmsnorm_fp8(RmsnormFp
     float g[8], y[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) y[e] = f[i][e], g[e] = 1.f;
-    if (a.gain) {
-      load8(a.gain, c, d, g);
+    if (gain) {
+      load8(gain, c, d, g);
 #pragma unroll
       for (int e = 0; e < 8; ++e) y[e] *= g[e];
     }
     // (the sum's and the product's roundings, of the value and of the largest, and the
     // factor's: 10 steps)
-    put_block<E8M0, LO ? kAgain : kAsIs>(a.o, row, c / kFp8Block, (c / 8) & 15, block_max<8>(y), m, y, 10, [&](double (&x)[8]) {
+    constexpr Fp8Look look = LO ? kAgain : BARE && sizeof(T) == 4 ? kFp32 : kAsIs;
+    put_block<E8M0, look>(a.o, row, c / kFp8Block, (c / 8) & 15, block_max<8>(y), m, y, 10, [&](double (&x)[8]) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) x[e] = ((double)f[i][e] + (double)lo[LO ? i : 0][e]) * (double)g[e] * r;
     });
@@ -281,10 +288,10 @@ hipError_t tiles_launch(const void* x, int rows, int cols, const Fp8Out& o, hipS
   return hipGetLastError();
 }
 
-template <typename T, bool E8M0, int NV>
+template <typename T, bool E8M0, int NV, bool BARE = false>
 hipError_t norm_launch_nv(const RmsnormFp8Args& a, int threads, hipStream_t s) {
   KernelTimer timer("rmsnorm_fp8", s);
-  hipExtLaunchKernelGGL((k_rmsnorm_fp8<T, E8M0, NV>), dim3(a.N), dim3(threads), 0, s, timer.start(), timer.stop(), 0, a);
+  hipExtLaunchKernelGGL((k_rmsnorm_fp8<T, E8M0, NV, BARE>), dim3(a.N), dim3(threads), 0, s, timer.start(), timer.stop(), 0, a);
   return hipGetLastError();
 }
 
@@ -293,6 +300,9 @@ hipError_t norm_launch(const RmsnormFp8Args& a, hipStream_t s) {
   const int chunks = a.o.ld / 8;
   const int nv = chunks <= 1024 ? 1 : chunks <= 2048 ? 2 : chunks <= 4096 ? 4 : 8;
   const int threads = ((chunks + nv - 1) / nv + kWaveSize - 1) / kWaveSize * kWaveSize;
+  if constexpr (!E8M0) {
+    if (nv == 1 && !a.residual && !a.gain) return norm_launch_nv<T, false, 1, true>(a, threads, s);
+  }
   switch (nv) {
     case 1: return norm_launch_nv<T, E8M0, 1>(a, threads, s);
     case 2: return norm_launch_nv<T, E8M0, 2>(a, threads, s);

@@ -139,3 +139,49 @@ def test_norm_of_infinite_sums(stype):
     for row in (0, 4):
         assert torch.equal(q[row].view(torch.uint8), want[0][row].view(torch.uint8))
         assert torch.equal(s[row].view(torch.uint8), want[1][row].view(torch.uint8))
+
+
+# ---- rows as they are -------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["x32", "x16"])
+def test_norm_of_bf16_numbers_alone(dtype):
+    """Without residual and gain the row's factor drops out of f 448 / A, whose bf16
+    operands 64 bits divide exactly wherever the quotient is the middle of two e4m3 values
+    (and otherwise lie 2^-17 of it away): every value is the nearest, middles to even."""
+    say("norm of bf16 numbers", dtype)
+    N, d = 501, 4096
+    x = torch.randn((N, d), generator=gen(51)).bfloat16().to(dtype)
+    q, s = P.rmsnorm_fp8(x.to(DEV))
+    f = x.double()
+    b = f.view(N, -1, BLOCK)
+    quot = (b * 448.0 / b.abs().amax(dim=2, keepdim=True)).view(N, d)
+    step = 2.0 ** (torch.frexp(quot)[1].double() - 4).clamp(min=-9.0)
+    assert torch.equal(q.cpu().float().double(), torch.round(quot / step) * step)
+    y = f / torch.sqrt(f.square().mean(dim=1, keepdim=True) + 1e-5)
+    top = y.view(N, -1, BLOCK).abs().amax(dim=2)
+    assert ((s.cpu().double() - top / 448.0).abs() <= 4 * 2.0 ** -24 * top / 448.0).all()
+
+
+def test_norm_of_bf16_numbers_alone_takes_no_longer_than_with_a_gain():
+    """It reads less and computes less (0.92 of the time; 1.65 where most waves
+    looked a second time at values on the middle of two)."""
+    say("norm of bf16 numbers, time")
+    x = [torch.randn((4096, 4096), device=DEV).bfloat16() for _ in range(6)]
+    gain = 1 + 0.1 * torch.randn(4096, device=DEV)
+    out = P.rmsnorm_fp8(x[0])
+
+    def us(g):
+        P.timer_reset()
+        P.timer_enable(True)
+        try:
+            for v in x:
+                P.rmsnorm_fp8(v, gain=g, out=out)
+            torch.cuda.synchronize()
+        finally:
+            P.timer_enable(False)
+        n, ms = P.timer_read()["rmsnorm_fp8"]
+        return ms / n * 1e3
+
+    both = [(us(None), us(gain)) for _ in range(8)]
+    alone, gained = min(b[0] for b in both), min(b[1] for b in both)
+    assert alone <= 1.3 * gained, (alone, gained)
