@@ -414,7 +414,9 @@ cats_status cats_silu_mul_fp8(const void* gate_up, int32_t dtype, int32_t N, int
  * outputs it reaches; scales may be any number of their type whose product of
  * two, which is formed first, is in fp32's range.  1 <= N, n <=
  * CATS_MAX_FP8_ROWS, 1 <= k <= CATS_MAX_FP8_COLS.  Workspace:
- * cats_linear_fp8_workspace_bytes(N, n, k). */
+ * cats_linear_fp8_workspace_bytes(N, n, k), of at most 48 MiB, which serves every
+ * call of up to N rows, n outputs and k columns.  Many calls need less and take a
+ * smaller one; CATS_ERR_WORKSPACE says what it would have to be. */
 size_t cats_linear_fp8_workspace_bytes(int32_t N, int32_t n, int32_t k);
 cats_status cats_linear_fp8(const void* xq, const void* xs, int32_t N, const void* wq, const void* wscale, int32_t n,
                             int32_t k, int32_t stype, const void* residual, void* y, int32_t ydtype, void* ws,

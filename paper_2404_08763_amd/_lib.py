@@ -663,6 +663,7 @@ def silu_mul_fp8(gate_up: torch.Tensor, t: float = 0.0, scale_dtype: torch.dtype
 
 
 def linear_fp8_workspace(N: int, n: int, k: int, device="cuda") -> torch.Tensor:
+    """Scratch memory for linear_fp8 calls of up to N rows, n outputs and k columns."""
     nbytes = int(raw().cats_linear_fp8_workspace_bytes(N, n, k))
     if nbytes == 0:
         raise ValueError("arguments outside the supported range")
@@ -674,7 +675,8 @@ def linear_fp8(xq: torch.Tensor, xs: torch.Tensor, wq: torch.Tensor, wscale: tor
                dtype: torch.dtype = torch.float32, ws: Optional[torch.Tensor] = None) -> torch.Tensor:
     """y = residual + x W^T for the rows (xq, xs) and the weight (wq, wscale), both
     as the quantising calls write them: xq [N, ld], wq [n, ld].  y [N, n] is fp32
-    or bf16 (`dtype`, or out's), the residual of y's type; out may be the residual."""
+    or bf16 (`dtype`, or out's), the residual of y's type; out may be the residual.
+    ws: linear_fp8_workspace's for this or a larger call (None: one for this call)."""
     N, ld = _two_dims(xq, "xq")
     n, ldw = _two_dims(wq, "wq")
     if ld != ldw or ld % FP8_BLOCK:

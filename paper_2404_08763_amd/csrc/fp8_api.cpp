@@ -65,6 +65,7 @@ cats_status launched(hipError_t e, void* stream, const char* what) {
 }
 
 constexpr size_t kWsAlign = 256;
+size_t ws_size(size_t bytes) { return bytes < kWsAlign ? kWsAlign : (bytes + kWsAlign - 1) / kWsAlign * kWsAlign; }
 
 bool linear_shape_ok(int32_t N, int32_t n, int32_t k) {
   return N >= 1 && N <= CATS_MAX_FP8_ROWS && n >= 1 && n <= CATS_MAX_FP8_ROWS && k >= 1 && k <= CATS_MAX_FP8_COLS;
@@ -137,8 +138,7 @@ cats_status cats_silu_mul_fp8(const void* gate_up, int32_t dtype, int32_t N, int
 
 size_t cats_linear_fp8_workspace_bytes(int32_t N, int32_t n, int32_t k) {
   if (!linear_shape_ok(N, n, k)) return 0;
-  const size_t bytes = cats::linear_fp8_partial_bytes(N, n, (int)blocks_of(k));
-  return bytes < kWsAlign ? kWsAlign : (bytes + kWsAlign - 1) / kWsAlign * kWsAlign;
+  return ws_size(cats::linear_fp8_partial_most(N, n, (int)blocks_of(k)));
 }
 
 cats_status cats_linear_fp8(const void* xq, const void* xs, int32_t N, const void* wq, const void* wscale, int32_t n,
@@ -162,7 +162,7 @@ cats_status cats_linear_fp8(const void* xq, const void* xs, int32_t N, const voi
       overlap(y, ny, wscale, blocks_of(n) * blocks_of(k) * scale_bytes(stype)) ||
       (residual && residual != y && overlap(y, ny, residual, ny)))
     return fail(CATS_ERR_RANGE, "y may be the residual, but must not overlap any other input");
-  const size_t need = cats_linear_fp8_workspace_bytes(N, n, k);
+  const size_t need = ws_size(cats::linear_fp8_partial_bytes(N, n, (int)blocks_of(k), ydtype == CATS_BF16, stype == CATS_SCALE_E8M0));
   if (!ws) return fail(CATS_ERR_WORKSPACE, "workspace is NULL");
   if (!aligned(ws, kWsAlign)) return fail(CATS_ERR_ALIGN, "workspace must be 256-byte aligned");
   if (ws_bytes < need) return fail(CATS_ERR_WORKSPACE, "workspace has %zu bytes, needs %zu", ws_bytes, need);

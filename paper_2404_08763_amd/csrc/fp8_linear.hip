@@ -947,6 +947,8 @@ struct LinearPlan {
 // unit and each of several, and what larger tiles take longer to start and end.
 constexpr int kTileStepF32 = 172, kTileStepE8m0 = 160, kTileStep = 210;
 constexpr int kMidParts[] = {1, 2, 3, 4, 5, 6, 8, 12, 16, 24};
+constexpr int kMidBlocks = 768;  // most blocks of a call in parts: three a compute unit
+inline bool mid_parts_ok(int S, int KB, int64_t blocks) { return S == 1 || (2 * S <= KB && blocks * S <= kMidBlocks); }
 constexpr int kMidStepOne[3] = {95, 97, 123}, kMidStepEach[3] = {46, 62, 99}, kMidStart[3] = {0, 40, 100};
 // The second launch; bytes of the parts' sums, written and read, and of weights, which two
 // blocks that run beside each other both fetch, in 1/100 us.
@@ -977,7 +979,7 @@ static LinearPlan linear_plan(int N, int n, int KB, bool bf16, bool e8m0) {
     const int64_t high = (N + rows - 1) / rows, blocks = columns * high;
     const int64_t fetch = columns * KB * (128 * 128) * (high > 1 ? 2 : 1);
     for (const int S : kMidParts) {
-      if (S > 1 && (2 * S > KB || blocks * S > 768)) break;  // (three a compute unit)
+      if (!mid_parts_ok(S, KB, blocks)) break;
       const int64_t all = blocks * S, rounds = (all + 255) / 256;
       // (a last round that fills part of the chip goes with less traffic beside it)
       const int64_t step = std::max<int64_t>(kMidStepOne[i], kMidStepEach[i] * (3 * 256 * rounds + all) / 1024);
@@ -995,14 +997,21 @@ static LinearPlan linear_plan(int N, int n, int KB, bool bf16, bool e8m0) {
 
 static int partial_pitch(int n) { return (n + 3) / 4 * 4; }
 
-size_t linear_fp8_partial_bytes(int N, int n, int KB) {
-  size_t most = 0;
-  for (int v = 0; v < 4; ++v) {
-    const LinearPlan p = linear_plan(N, n, KB, (v & 1) != 0, (v & 2) != 0);
-    const size_t bytes = p.S > 1 ? (size_t)p.S * N * partial_pitch(n) * sizeof(float) : 0;
-    if (bytes > most) most = bytes;
-  }
-  return most;
+size_t linear_fp8_partial_bytes(int N, int n, int KB, bool bf16, bool e8m0) {
+  const LinearPlan p = linear_plan(N, n, KB, bf16, e8m0);
+  return p.S > 1 ? (size_t)p.S * N * partial_pitch(n) * sizeof(float) : 0;
+}
+
+// The plan's own parts go up and down with N and n (4096 -> 4096: 16 MB at 256 rows, none
+// at 512), so the bound is on what any of the smaller calls may take: the most parts that
+// KB allows, and kMidBlocks blocks of 128 outputs and the most rows that N allows.
+size_t linear_fp8_partial_most(int N, int n, int KB) {
+  if (N <= 16 || (N <= 32 && KB <= 2 * kStreamWaves)) return 0;
+  int parts = 1;
+  for (const int S : kMidParts) parts = mid_parts_ok(S, KB, 1) ? S : parts;
+  if (parts == 1) return 0;
+  const int rows = N <= 32 ? 32 : N <= 64 ? 64 : 128;
+  return std::min((size_t)parts * N * partial_pitch(n), (size_t)kMidBlocks * 128 * rows) * sizeof(float);
 }
 
 hipError_t launch_linear_fp8(LinearFp8Args a, hipStream_t s) {

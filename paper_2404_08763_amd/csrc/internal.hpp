@@ -270,8 +270,10 @@ hipError_t launch_quantize_fp8(const void* x, int bf16, int rows, int cols, int 
 hipError_t launch_silu_fp8(const void* gu, int bf16, int N, int m, float t, const Fp8Out& o, hipStream_t s);
 hipError_t launch_rmsnorm_fp8(const RmsnormFp8Args& a, int bf16, hipStream_t s);
 hipError_t launch_linear_fp8(LinearFp8Args a, hipStream_t s);
-// Bytes of the partial sums that a call of that size may need (of either output type).
-size_t linear_fp8_partial_bytes(int N, int n, int KB);
+// Bytes of the partial sums of a call, and at most of any call of up to N rows, n outputs and
+// KB column blocks.
+size_t linear_fp8_partial_bytes(int N, int n, int KB, bool bf16, bool e8m0);
+size_t linear_fp8_partial_most(int N, int n, int KB);
 
 // Optional per-kernel timing (cats_timer_*): while the timer is enabled a
 // KernelTimer hands out a pair of HIP events that the launch (through
