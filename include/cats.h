@@ -351,8 +351,9 @@ cats_status cats_rmsnorm(const float* x, float* xn, int32_t B, int32_t d, float 
  * smallest 2^e with a <= 448 * 2^e and e >= -126, and 1 where a is 0; q is the
  * e4m3 value nearest to the element times 448 / a or 2^-e (ties to even), as 64
  * bits give them; fp32's roundings may take the other of two about equally near
- * ones where q is below 2^-6 or the scale 2^-126, and for RMSNorm of more than
- * 8192 columns.  An infinite or NaN element becomes e4m3's NaN; the block's other
+ * ones where q is below 2^-6, a below 2^-100 or the scale 2^-126, and for RMSNorm of
+ * more than 8192 columns.  fp32 scales are within a few of fp32's steps of a / 448.
+ * An infinite or NaN element becomes e4m3's NaN; the block's other
  * elements are what they are without it.
  * All four calls are enqueue only and may be captured in a graph. */
 #define CATS_FP8_BLOCK 128
@@ -394,7 +395,8 @@ cats_status cats_rmsnorm_fp8(const void* x, int32_t dtype, const float* residual
  *   v = SiLU(g),  h = v * u where |v| >= t, else 0,  q, scale = quantise(h)
  * with one scale per row and CATS_FP8_BLOCK neurons.  t >= 0 as in
  * cats_mlp_forward (NaN v is kept; t = 0 keeps every neuron, t = +inf no
- * finite one).  SiLU(g) of less than 1.2e-36 may be 0. */
+ * finite one), |v| >= t as 64 bits give it, and u of a neuron below t counts for nothing,
+ * infinite or NaN.  SiLU(g) of less than 1.2e-36 may be 0. */
 cats_status cats_silu_mul_fp8(const void* gate_up, int32_t dtype, int32_t N, int32_t m, float t, int32_t stype, void* q,
                               void* scale, void* stream);
 
@@ -409,7 +411,7 @@ cats_status cats_silu_mul_fp8(const void* gate_up, int32_t dtype, int32_t N, int
  * For fp32 y the products are exact and summed in fp32.  For bf16 y and many
  * rows the 8-bit matrix instructions multiply: they cut each product at 2^-13 of
  * the power of two in the largest of its group of eight columns, below bf16's
- * rounding of sums whose terms do not cancel.
+ * rounding of sums whose terms do not cancel (fp32 y, rounded by the caller, has none of it).
  * xq, wq, y and residual 16-byte aligned; ws overlaps nothing.  NaN in q or a scale makes NaN of the
  * outputs it reaches; scales may be any number of their type whose product of
  * two, which is formed first, is in fp32's range.  1 <= N, n <=

@@ -676,6 +676,8 @@ def linear_fp8(xq: torch.Tensor, xs: torch.Tensor, wq: torch.Tensor, wscale: tor
     """y = residual + x W^T for the rows (xq, xs) and the weight (wq, wscale), both
     as the quantising calls write them: xq [N, ld], wq [n, ld].  y [N, n] is fp32
     or bf16 (`dtype`, or out's), the residual of y's type; out may be the residual.
+    Products are exact for fp32 y; for bf16 y of many rows they are cut at 2^-13 of the
+    largest of their group of eight columns.
     ws: linear_fp8_workspace's for this or a larger call (None: one for this call)."""
     N, ld = _two_dims(xq, "xq")
     n, ldw = _two_dims(wq, "wq")

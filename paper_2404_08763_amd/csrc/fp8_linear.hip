@@ -146,7 +146,9 @@ __device__ __forceinline__ void put_staged(const LinearFp8Args& a, f32x4* stage,
 // instruction reads whole 128-byte lines, of eight rows (rows r and r + 8 in two
 // loads, then lanes r and r + 8 exchange halves: 4096 -> 22016 of one row 16.6 us,
 // 22.1 with 64 bytes of 16 rows).  4096 -> 22016: 5.4 TB/s, launch included, of
-// the 7.2 that a large plain read reaches.
+// the 7.2 that a large plain read reaches.  Short streams pay the latencies one after the
+// other: 4096 -> 6144 is 192 blocks of two tiles, the second asked for when the first is there
+// (7.6 us, 3.3 TB/s).  With C = 4 six to nine registers spill (8192 -> 28672 47 us, 5.0 TB/s).
 constexpr int kStreamWaves = 16;
 template <int C, int NB, bool E8M0, bool RES>
 __global__ __launch_bounds__(64 * kStreamWaves) void k_fp8_stream(LinearFp8Args a, int CT) {
@@ -274,7 +276,9 @@ static hipError_t launch_stream(const LinearFp8Args& a, hipStream_t s) {
 
 // Up to 16 rows of more column blocks than that: a block owns 16 outputs, its
 // waves split the column blocks the same way, weights and x two column blocks
-// ahead in registers.
+// ahead in registers.  14336 -> 4096 of 16 rows 20 us, 11008 -> 4096 of one row 13 (2.9 and 3.4
+// TB/s; nothing is fetched twice): a wave has five to seven column blocks, two of them under
+// way, between the first loads of its block and the sum over 16 waves.
 template <bool E8M0>
 __global__ __launch_bounds__(64 * kStreamWaves) void k_fp8_split(LinearFp8Args a) {
   constexpr int W = kStreamWaves, D = 2;
@@ -406,9 +410,12 @@ constexpr int kTileGroup = 6;  // (whole columns: 5% slower for 2048 rows 4096 -
 //
 // bf16 outputs: 256 x 256, the 8-bit instructions, one a tile and step, E8M0 scales
 // applied by them, fp32 ones on the vector ALUs, whose sums lie between the
-// products.  Bound by the matrix cores (0.6 of their time with E8M0), the sums and
-// what of the loads does not overlap: 4096 rows 14336 -> 4096 175 us, 2.7 PFLOP/s
-// (fp32 scales 226 us, 2.1), where the library's product of one scale for all takes 153.
+// products.  Bound by what of the reading phases, loads and sums does not overlap with the
+// products: of a busy compute unit's cycles the matrix cores work 0.66 with E8M0 scales and
+// 0.43 with fp32 ones, the vector ALUs 0.35 and 0.40 (fp32 scales are 128 multiply-adds a wave
+// and step, half as long as its 32 products, and use products three instructions
+// back).  4096 rows 14336 -> 4096 172 to 175 us, 2.8 PFLOP/s (fp32 scales 225 us, 2.1), where the
+// library's product of one scale for all takes 153.
 // EXACT, fp32 outputs: 256 x 128, the bf16 instructions; operands are widened in the
 // reading phase, under the other group's products (in the multiplying phase:
 // 410 us).  The same size 371 to 412 us by the card, 1.17 to 1.30 PFLOP/s; the library's bf16 product, whose
@@ -735,7 +742,7 @@ static hipError_t launch_tile(const LinearFp8Args& a, hipStream_t s) {
 // a step.  Bound by a step's chain of reads, widening and products (0.9, 1.0 and 1.2 us of
 // a lone block of 32, 64 and 128 rows, 0.5, 0.6 and 1.0 each of several on a compute unit),
 // by the parts' traffic and the second launch where there are many parts: 300 rows
-// 4096 -> 4096 24 us, 101 rows 7001 -> 2857 18, 312 rows 256 -> 3106 6.7.
+// 4096 -> 4096 23 us, 101 rows 7001 -> 2857 17, 312 rows 256 -> 3106 6.7.
 template <int TN> struct MidGeom;
 template <> struct MidGeom<128> { static constexpr int WN = 2, MI = 2, NB = 2; };  // waves along x's rows, 32 x 32 tiles of a wave
 template <> struct MidGeom<64> { static constexpr int WN = 2, MI = 2, NB = 1; };

@@ -6,8 +6,9 @@
 // lane's registers between the load and the 8-byte store of its e4m3 values.
 // All of them are bound by memory, each input read once and each output written
 // once, and reach the rate of a large copy (5.1 TB/s): the gate of 2048 x 14336 in
-// bf16 148 MB in 29.0 us, 11008 x 4096 bf16 weights 135 MB in 27.4, RMSNorm of 4096 x 4096
-// bf16 with the residual and its new value 185 MB in 37.0.
+// bf16 148 MB in 29.1 us (its vector instructions take about as long), 11008 x 4096 bf16
+// weights 135 MB in 27.5, RMSNorm of 4096 x 4096 bf16 with the residual and its new value 185
+// MB in 36.8.
 #include "fp8.hpp"
 #include "internal.hpp"
 
@@ -168,8 +169,8 @@ __global__ __launch_bounds__(1024, NV == 1 ? 8 : 4) void k_rmsnorm_fp8(RmsnormFp
   const size_t row = blockIdx.x;
   const T* xr = static_cast<const T*>(a.x) + row * d;
   // What the additions round off is kept for values next to a middle.  Rows of more than
-  // 8192 columns have no registers for it without fewer waves (2048 rows of 12288: 56 us, 48
-  // without), and no second look.
+  // 8192 columns have no registers for it without fewer waves (2048 rows of 12288, bf16 with
+  // residual: 56 us, 48 without), and no second look.
   constexpr bool LO = NV == 1 && !BARE;
   float f[NV][8], lo[LO ? NV : 1][8] = {};
   // The row's factor reaches q with E8M0 scales alone: there the squares are those of 64
