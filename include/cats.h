@@ -424,6 +424,105 @@ cats_status cats_linear_fp8(const void* xq, const void* xs, int32_t N, const voi
                             int32_t k, int32_t stype, const void* residual, void* y, int32_t ydtype, void* ws,
                             size_t ws_bytes, void* stream);
 
+/* ---- around attention --------------------------------------------------------
+ * From the Q/K/V projection (cats_linear_fp8, cats_sparse_input_gemv) to the
+ * output projection: norms and rotation of the heads, a cache of keys and values
+ * in 4 bits, attention over it.  All calls are enqueue only and may be
+ * captured in a graph; their lengths, tables, positions and slots are read on
+ * the device, so a captured call serves other ones.  They are checked there:
+ * nothing they hold makes a call read or write outside its arguments. */
+#define CATS_MAX_KV_ROWS (1 << 20)
+#define CATS_MAX_KV_HEADS 1024
+#define CATS_MAX_KV_TOKENS (1 << 30)
+#define CATS_MAX_KV_PITCH (1 << 30)
+
+/* Norms of queries and keys for each head, with the position rotation in the
+ * same pass.  A row of qkv (dev [N x ld] fp32 or bf16, ld >= (hq + hkv) d a
+ * multiple of 8) begins with hq query heads of d columns, then hkv key heads; what
+ * follows (the values) is not read.  For each head x:
+ *   n = x / sqrt(mean(x^2) + eps) * gain   (norm; else n = x)
+ *   the pairs (n[i], n[i + rot/2]), or with `interleaved` (n[2i], n[2i + 1]), i <
+ *   rot/2, are turned by the angle a = pos[row] * freq[i]:
+ *   (u, w) -> (u cos a - w sin a, w cos a + u sin a); columns from rot on stay.
+ *   gain_q, gain_k  dev [d] fp32, or NULL: 1 (read with norm only)
+ *   pos, freq       dev [N] int32, dev [rot/2] fp32 (not read if rot is 0); the
+ *                   product is taken in 64 bits, so positions far out lose nothing
+ *   q, k            dev [N x hq x d], [N x hkv x d], odtype fp32 or bf16, rounded
+ *                   once; must not overlap the inputs
+ * A head whose squares leave fp32's range becomes 0 (as cats_rmsnorm's rows).
+ * 1 <= N <= CATS_MAX_KV_ROWS, d a multiple of 8 up to 512, rot a multiple of 8
+ * up to d; all but pos 16-byte aligned. */
+cats_status cats_qk_norm_rope(const void* qkv, int32_t dtype, int64_t ld, int32_t N, int32_t hq, int32_t hkv, int32_t d,
+                              int32_t norm, const float* gain_q, const float* gain_k, float eps, const int32_t* pos,
+                              const float* freq, int32_t rot, int32_t interleaved, void* q, void* k, int32_t odtype,
+                              void* stream);
+
+/* A cache of keys and values in 4 bits: e2m1 codes (OCP FP4: sign, 0 .5 1 1.5 2 3
+ * 4 6) with an E8M0 scale for each 32 columns of a token, d + d/16 bytes for a
+ * token's key and value of a head.  It is held in pages of `page` tokens (16 to
+ * 256, a multiple of 16) of all heads, in any order: slot s is token s % page of
+ * page s / page.  A page holds, for each head and 16 tokens, a record of 17 d
+ * bytes: keys (token t, column c in byte t d/2 + c/2, even columns in the low
+ * half), values (byte 8 d + ((t/4 * 16 + n) * 4 + t % 4) * d/32 + r/2, n = c / (d/16), r = c
+ * % (d/16)), the keys' scales (byte 16 d + t d/32 + c/32) and the values'
+ * (16 d + d/2 + (t/4 * d/32 + c/32) * 4 + t % 4).  It needs no clearing: what was not
+ * written is not used.  data is 16-byte aligned, d 64, 128 or 256, pages * page
+ * at most CATS_MAX_KV_TOKENS. */
+typedef struct {
+  void* data;
+  int32_t pages;
+  int32_t page;
+  int32_t heads;
+  int32_t d;
+} cats_kv_cache;
+
+/* Bytes of a cache's data; 0 outside the limits.  Pure host arithmetic. */
+size_t cats_kv_cache_bytes(int32_t pages, int32_t page, int32_t heads, int32_t d);
+
+/* Quantise N rows of keys and values (dev [N x ldk], [N x ldv] fp32 or bf16, heads * d
+ * columns from a 16-byte aligned one on, pitches multiples of 8: the columns of a
+ * Q/K/V projection's rows as they are) into the slots of the cache.  A block of 32
+ * columns with largest magnitude a takes the smallest scale 2^e with a <= 6 * 2^e, e in
+ * [-125, 125] (1 if a is 0), and each element the code nearest to it over
+ * 2^e (ties to the even code; beyond 6 * 2^125, 6).  A block with an infinity
+ * or NaN takes the scale NaN and reads back as NaN.
+ * A row whose slot is outside [0, pages * page) is left out, as padding is.  The
+ * slots of one call must differ: one that two rows share holds parts of both. */
+cats_status cats_kv_write(const cats_kv_cache* cache, const void* k, int64_t ldk, const void* v, int64_t ldv, int32_t dtype,
+                          const int32_t* slots, int32_t N, void* stream);
+
+/* Read N slots back, exactly: k, v dev [N x heads x d], fp32 or bf16.  Rows whose
+ * slot is outside the cache are left as they were. */
+cats_status cats_kv_read(const cats_kv_cache* cache, const int32_t* slots, int32_t N, void* k, void* v, int32_t dtype,
+                         void* stream);
+
+/* Causal attention of query rows over the cache:
+ *   out[r, h] = sum_j softmax_j(scale * q[r, h] . k_j) v_j
+ * over the keys j in [0, pos] (with window > 0: (pos - window, pos]) of the row's
+ * sequence, with key head h / (hq / heads).
+ *   q, out   dev [N x hq x d], both fp32 or both bf16; must not overlap
+ *   table    dev [B x width] int32: page w of sequence b holds its tokens [w page,
+ *            (w + 1) page); entries behind its length are not read
+ *   lens     dev [B] int32: tokens of each sequence, the rows' own among them
+ *            (written before); taken as within [0, width * page]
+ *   q_start  dev [B + 1] int32: rows [q_start[b], q_start[b + 1]) are sequence b's
+ *            last ones, row i at pos = lens[b] - count + i; non-decreasing, from 0
+ *            or more to N or less.  NULL: one row for each sequence, N = B.
+ * A row that sees no key (pos < 0) becomes 0; rows that belong to no sequence are
+ * left as they were.  A row that sees a token of a page outside [0, pages) becomes NaN.
+ * Masked tokens have no effect, whatever the cache holds for them.
+ * Products of q and the cache's values are exact and summed in fp32, as is the
+ * softmax; its weights enter the second product with 16 bits for bf16 rows and
+ * 24 for fp32 rows.  A row's bits may depend on the other sequences of the
+ * call (how the keys are shared out), but not from run to run.
+ * Workspace: cats_kv_attention_workspace_bytes(N, B, hq, heads, d), which serves
+ * every call of up to as many rows and sequences of the same heads.
+ * 1 <= N, B <= CATS_MAX_KV_ROWS, hq a multiple of heads, scale > 0, window >= 0. */
+size_t cats_kv_attention_workspace_bytes(int32_t N, int32_t B, int32_t hq, int32_t heads, int32_t d);
+cats_status cats_kv_attention(const void* q, int32_t dtype, int32_t N, int32_t hq, const cats_kv_cache* cache,
+                              const int32_t* table, int32_t width, const int32_t* lens, const int32_t* q_start, int32_t B,
+                              float scale, int32_t window, void* out, void* ws, size_t ws_bytes, void* stream);
+
 /* Attainable read bandwidth (a measurement aid; nothing of the method):
  * streams `bytes` of device memory at `buf` (16-byte aligned, a positive
  * multiple of 16, at most 1 GiB) with the 16-byte non-temporal loads the

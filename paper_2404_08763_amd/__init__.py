@@ -20,6 +20,11 @@ from ._lib import (  # noqa: F401
     calib_activations,
     calibrate_threshold,
     fp8_ld,
+    kv_attention,
+    kv_attention_workspace,
+    kv_cache,
+    kv_read,
+    kv_write,
     layer_from_math,
     lib_path,
     linear_fp8,
@@ -29,6 +34,7 @@ from ._lib import (  # noqa: F401
     mlp_forward_topk,
     mlp_forward_unfused,
     pack_weights,
+    qk_norm_rope,
     quantize_fp8,
     raw,
     Stack,

@@ -50,6 +50,11 @@ class _Aux(ctypes.Structure):
                 ("active_v", ctypes.c_void_p), ("active_h", ctypes.c_void_p)]
 
 
+class _KvCache(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("pages", ctypes.c_int32), ("page", ctypes.c_int32),
+                ("heads", ctypes.c_int32), ("d", ctypes.c_int32)]
+
+
 _vp = ctypes.c_void_p
 _i32 = ctypes.c_int32
 _i64 = ctypes.c_int64
@@ -92,6 +97,14 @@ _SIGNATURES = {
     "cats_silu_mul_fp8": ([_vp, _i32, _i32, _i32, _f32, _i32, _vp, _vp, _vp], _i32),
     "cats_linear_fp8_workspace_bytes": ([_i32, _i32, _i32], _sz),
     "cats_linear_fp8": ([_vp, _vp, _i32, _vp, _vp, _i32, _i32, _i32, _vp, _vp, _i32, _vp, _sz, _vp], _i32),
+    "cats_qk_norm_rope": ([_vp, _i32, _i64, _i32, _i32, _i32, _i32, _i32, _vp, _vp, _f32, _vp, _vp, _i32, _i32, _vp,
+                           _vp, _i32, _vp], _i32),
+    "cats_kv_cache_bytes": ([_i32, _i32, _i32, _i32], _sz),
+    "cats_kv_write": ([ctypes.POINTER(_KvCache), _vp, _i64, _vp, _i64, _i32, _vp, _i32, _vp], _i32),
+    "cats_kv_read": ([ctypes.POINTER(_KvCache), _vp, _i32, _vp, _vp, _i32, _vp], _i32),
+    "cats_kv_attention_workspace_bytes": ([_i32, _i32, _i32, _i32, _i32], _sz),
+    "cats_kv_attention": ([_vp, _i32, _i32, _i32, ctypes.POINTER(_KvCache), _vp, _i32, _vp, _vp, _i32, _f32, _i32,
+                           _vp, _vp, _sz, _vp], _i32),
     "cats_stream_read": ([_vp, _sz, _i32, _i32, _i32, _vp, _vp], _i32),
     "cats_timer_enable": ([_i32], _i32),
     "cats_timer_reset": ([], _i32),
@@ -707,6 +720,192 @@ def linear_fp8(xq: torch.Tensor, xs: torch.Tensor, wq: torch.Tensor, wscale: tor
         ws = linear_fp8_workspace(N, n, ld, device=xq.device)
     _check(raw().cats_linear_fp8(xq.data_ptr(), xs.data_ptr(), N, wq.data_ptr(), wscale.data_ptr(), n, ld, st,
                                  _ptr(residual), out.data_ptr(), yt, ws.data_ptr(), ws.numel(), _stream()))
+    return out
+
+
+# ---- around attention ---------------------------------------------------------
+# Norms and rotation of the heads, the cache of keys and values in 4 bits, and
+# attention over it.  A cache is a uint8 tensor [pages, heads, page / 16, 17 d]: a
+# record of 17 d bytes for 16 tokens of a head (cats.h has its layout).
+
+_KV_RECORD = 17  # bytes of a record for each column
+
+
+def kv_cache(pages: int, heads: int, d: int, page: int = 64, device="cuda") -> torch.Tensor:
+    """Memory for a cache of `pages` pages of `page` tokens (a multiple of 16 up to
+    256) of `heads` key heads of d = 64, 128 or 256 columns.  Not cleared: what is
+    not written is not used."""
+    if not raw().cats_kv_cache_bytes(pages, page, heads, d):
+        raise ValueError("arguments outside the supported range")
+    return torch.empty((pages, heads, page // 16, _KV_RECORD * d), dtype=torch.uint8, device=device)
+
+
+def _kv(cache: torch.Tensor, device: int):
+    """A cache's C structure, its heads and its columns."""
+    if cache.dim() != 4 or cache.shape[3] % _KV_RECORD:
+        raise ValueError(f"cache must be [pages, heads, page / 16, 17 d], has shape {list(cache.shape)}")
+    if cache.dtype is not torch.uint8 or cache.get_device() != device or not cache.is_contiguous():
+        _refuse("cache", cache, torch.uint8, device)
+    pages, heads, groups, rec = cache.shape
+    d = rec // _KV_RECORD
+    return _KvCache(cache.data_ptr(), pages, 16 * groups, heads, d), heads, d
+
+
+def _on(name: str, t: Optional[torch.Tensor], dtype: torch.dtype, device: int) -> None:
+    if t is not None and (t.dtype is not dtype or t.get_device() != device or not t.is_contiguous()):
+        _refuse(name, t, dtype, device)
+
+
+def _pitched(name: str, t: torch.Tensor, cols: int, device: int) -> int:
+    """The pitch of rows [N, cols] or [N, heads, d] whose columns are dense."""
+    if t.dtype is not torch.float32 and t.dtype is not torch.bfloat16:
+        raise ValueError(f"{name} must be torch.float32 or torch.bfloat16, got {t.dtype}")
+    if t.get_device() != device:
+        _refuse(name, t, t.dtype, device)
+    if t.stride(-1) != 1 or (t.dim() == 3 and t.shape[1] > 1 and t.stride(1) != t.shape[2]):
+        raise ValueError(f"{name}'s rows must be dense")
+    return t.stride(0) if t.shape[0] > 1 else (cols + 7) // 8 * 8
+
+
+def qk_norm_rope(qkv: torch.Tensor, heads: int, kv_heads: int, d: int, pos: Optional[torch.Tensor] = None,
+                 freq: Optional[torch.Tensor] = None, norm: bool = False, gain_q: Optional[torch.Tensor] = None,
+                 gain_k: Optional[torch.Tensor] = None, eps: float = 1e-5, interleaved: bool = False,
+                 dtype: Optional[torch.dtype] = None, out=None):
+    """(q [N, heads, d], k [N, kv_heads, d]) of qkv's rows (fp32 or bf16; a row's
+    query heads, then its key heads; what follows is not read; rows may be
+    strided): each head RMS-normed with gain_q or gain_k [d] fp32 (`norm`), then the
+    first 2 len(freq) columns turned by pos [N] int32 times freq [rot / 2] fp32
+    (freq None: none), in pairs (i, i + rot / 2) or, `interleaved`, (2 i, 2 i + 1).
+    dtype: of q and k (None: qkv's); out: a (q, k) pair to write to."""
+    N, cols = _two_dims(qkv, "qkv")
+    if cols < (heads + kv_heads) * d:
+        raise ValueError(f"qkv must have {(heads + kv_heads) * d} columns or more, has {cols}")
+    if not qkv.is_cuda:
+        raise ValueError("qkv must be a device tensor")
+    if out is None:
+        dtype = qkv.dtype if dtype is None else dtype
+        out = tuple(torch.empty((N, h, d), dtype=dtype, device=qkv.device) for h in (heads, kv_heads))
+    q, k = out
+    dtype = q.dtype
+    device = _device()
+    ld = _pitched("qkv", qkv, cols, device)
+    _shape_is(q, (N, heads, d), "q")
+    _shape_is(k, (N, kv_heads, d), "k")
+    rot = 0
+    if freq is not None:
+        rot = 2 * freq.shape[0]
+        if pos is None:
+            raise ValueError("freq needs pos")
+        _shape_is(freq, (rot // 2,), "freq")
+        _shape_is(pos, (N,), "pos")
+        _on("freq", freq, torch.float32, device)
+        _on("pos", pos, torch.int32, device)
+    for name, t in (("gain_q", gain_q), ("gain_k", gain_k)):
+        if t is not None:
+            if not norm:
+                raise ValueError(f"{name} needs norm=True")
+            _shape_is(t, (d,), name)
+            _on(name, t, torch.float32, device)
+    _on("q", q, dtype, device)
+    _on("k", k, dtype, device)
+    _check(raw().cats_qk_norm_rope(qkv.data_ptr(), _wdtype(qkv.dtype), ld, N, heads, kv_heads, d, 1 if norm else 0,
+                                   _ptr(gain_q), _ptr(gain_k), eps, _ptr(pos) if rot else None, _ptr(freq), rot,
+                                   1 if interleaved else 0, q.data_ptr(), k.data_ptr(), _wdtype(dtype), _stream()))
+    return q, k
+
+
+def _slots_of(slots: torch.Tensor, device: int) -> int:
+    if slots.dim() != 1:
+        raise ValueError(f"slots must have one dimension, got shape {list(slots.shape)}")
+    _on("slots", slots, torch.int32, device)
+    return slots.shape[0]
+
+
+def kv_write(cache: torch.Tensor, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor) -> None:
+    """Quantises rows of keys and values ([N, heads, d] or [N, heads d] fp32 or bf16,
+    each row dense, rows strided as they like) into the cache's slots [N] int32
+    (token s % page of page s // page; outside the cache: the row is left out).  The
+    slots inside the cache must differ."""
+    device = _device()
+    c, heads, d = _kv(cache, device)
+    N = _slots_of(slots, device)
+    for name, t in (("k", k), ("v", v)):
+        if t.shape != (N, heads, d) and t.shape != (N, heads * d):
+            raise ValueError(f"{name} must be {[N, heads, d]} or {[N, heads * d]}, has shape {list(t.shape)}")
+    if k.dtype != v.dtype:
+        raise ValueError(f"k and v must have one type, got {k.dtype} and {v.dtype}")
+    ldk, ldv = _pitched("k", k, heads * d, device), _pitched("v", v, heads * d, device)
+    _check(raw().cats_kv_write(ctypes.byref(c), k.data_ptr(), ldk, v.data_ptr(), ldv, _wdtype(k.dtype), slots.data_ptr(),
+                               N, _stream()))
+
+
+def kv_read(cache: torch.Tensor, slots: torch.Tensor, dtype: torch.dtype = torch.bfloat16, out=None):
+    """(k, v) [N, heads, d] of the cache's slots [N] int32, fp32 or bf16, both exact.
+    Rows whose slot is outside the cache are left as they are in `out` (without
+    `out`: undefined)."""
+    device = _device()
+    c, heads, d = _kv(cache, device)
+    N = _slots_of(slots, device)
+    if out is None:
+        out = tuple(torch.empty((N, heads, d), dtype=dtype, device=cache.device) for _ in range(2))
+    k, v = out
+    for name, t in (("k", k), ("v", v)):
+        _shape_is(t, (N, heads, d), name)
+        _on(name, t, k.dtype, device)
+    _check(raw().cats_kv_read(ctypes.byref(c), slots.data_ptr(), N, k.data_ptr(), v.data_ptr(), _wdtype(k.dtype), _stream()))
+    return k, v
+
+
+def kv_attention_workspace(N: int, B: int, heads: int, kv_heads: int, d: int, device="cuda") -> torch.Tensor:
+    """Scratch memory for kv_attention calls of up to N rows of B sequences."""
+    nbytes = int(raw().cats_kv_attention_workspace_bytes(N, B, heads, kv_heads, d))
+    if nbytes == 0:
+        raise ValueError("arguments outside the supported range")
+    return torch.empty(nbytes, dtype=torch.uint8, device=device)
+
+
+def kv_attention(q: torch.Tensor, cache: torch.Tensor, table: torch.Tensor, lens: torch.Tensor,
+                 q_start: Optional[torch.Tensor] = None, scale: Optional[float] = None, window: int = 0,
+                 out: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Causal attention of q [N, heads, d] (fp32 or bf16; out has its type) over the
+    cache: table [B, width] int32 has each sequence's pages, lens [B] int32 its
+    tokens (the rows' own among them), q_start [B + 1] int32 its rows, which are its
+    last ones (None: one row for each sequence).  scale: None is d ** -0.5; window:
+    0, or how many tokens a row sees.  Rows that see no key become 0; rows of no
+    sequence are left as they are in `out` (without `out`: undefined).
+    ws: kv_attention_workspace's for this or a larger call (None: one for this call)."""
+    if q.dim() != 3:
+        raise ValueError(f"q must be [N, heads, d], got shape {list(q.shape)}")
+    device = _device()
+    c, kv_heads, d = _kv(cache, device)
+    N, heads, dq = q.shape
+    if dq != d:
+        raise ValueError(f"q's heads have {dq} columns, the cache's {d}")
+    B, width = _two_dims(table, "table")
+    _shape_is(lens, (B,), "lens")
+    if q_start is not None:
+        _shape_is(q_start, (B + 1,), "q_start")
+    elif N != B:
+        raise ValueError(f"without q_start q must have a row for each of {B} sequences, has {N}")
+    dtype = q.dtype
+    dt = _wdtype(dtype)
+    if out is None:
+        if not q.is_cuda:
+            raise ValueError("q must be a device tensor")
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)
+    else:
+        _shape_is(out, (N, heads, d), "out")
+    _on("q", q, dtype, device)
+    _on("out", out, dtype, device)
+    _on("table", table, torch.int32, device)
+    _on("lens", lens, torch.int32, device)
+    _on("q_start", q_start, torch.int32, device)
+    _on("ws", ws, torch.uint8, device)
+    if ws is None:
+        ws = kv_attention_workspace(N, B, heads, kv_heads, d, device=q.device)
+    _check(raw().cats_kv_attention(q.data_ptr(), dt, N, heads, ctypes.byref(c), table.data_ptr(), width, lens.data_ptr(),
+                                   _ptr(q_start), B, d ** -0.5 if scale is None else scale, window, out.data_ptr(),
+                                   ws.data_ptr(), ws.numel(), _stream()))
     return out
 
 

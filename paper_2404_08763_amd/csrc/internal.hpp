@@ -275,6 +275,66 @@ hipError_t launch_linear_fp8(LinearFp8Args a, hipStream_t s);
 size_t linear_fp8_partial_bytes(int N, int n, int KB, bool bf16, bool e8m0);
 size_t linear_fp8_partial_most(int N, int n, int KB);
 
+// Around attention (qk_rope.hip, kv_cache.hip, kv_attention.hip).
+struct QkRopeArgs {
+  const void* x;         // [N x ld]: a row's hq query heads, then its hkv key heads, d columns each
+  size_t ld;
+  const int* pos;        // [N]
+  const float* freq;     // [rot / 2]
+  const float* gq;       // [d] or null
+  const float* gk;
+  void* q;               // [N x hq x d]
+  void* k;               // [N x hkv x d]
+  int N, hq, hkv, d, rot, norm, interleaved;
+  float eps;
+  int passes, chunks;    // passes of a wave, waves of a row (set by the launcher)
+};
+hipError_t launch_qk_rope(QkRopeArgs a, bool xbf16, bool ybf16, hipStream_t s);
+
+struct KvRowsArgs {
+  uint8_t* cache;        // [pages x heads x page / 16] records (kv4.hpp)
+  const int* slots;      // [rows]; a row whose slot is outside [0, tokens) is left out
+  int tokens;            // pages * page
+  int page, heads, rows;
+  const void* k;         // write: [rows x ldk], [rows x ldv]
+  const void* v;
+  size_t ldk, ldv;
+  void* k_out;           // read: [rows x heads x d]
+  void* v_out;
+};
+hipError_t launch_kv_rows(bool write, bool bf16, int d, const KvRowsArgs& a, hipStream_t s);
+
+struct KvPlanEntry {     // a tile of query rows of one sequence
+  int b, row0;           // its first row, counted over the sequence's queries and a key head's query heads
+};
+struct KvAttentionArgs {
+  const void* q;         // [N x hq x d]
+  void* out;
+  const uint8_t* cache;
+  const int* table;      // [B x width]
+  const int* lens;       // [B]
+  const int* q_start;    // [B + 1], or null: one query for each sequence
+  int N, B, hq, hkv, pages, width;
+  int groups;            // records of a page
+  uint32_t magic;        // ceil(2^31 / groups)
+  int limit;             // tokens a row of the table reaches
+  float c;               // scale * log2(e)
+  int window;            // 0: none
+  int tiles;             // without a plan: tiles of a sequence's query heads
+  int blocks;
+  // workspace
+  int* head;             // plan: tiles, units of a head
+  KvPlanEntry* plan;
+  int* prefix;           // units in front of each tile
+  int* first;            // [B + 1] first tile of each sequence
+  int4* desc;            // [blocks] the sum that begins in each block
+  float* part;           // [blocks x 2] partial sums
+};
+// Workspace of a call, and at most of any call of up to N rows and B sequences.
+size_t kv_attention_bytes(int N, int B, int hq, int hkv, int d, bool bf16, bool planned);
+size_t kv_attention_most(int N, int B, int hq, int hkv, int d);
+hipError_t launch_kv_attention(KvAttentionArgs a, int d, bool bf16, hipStream_t s);
+
 // Optional per-kernel timing (cats_timer_*): while the timer is enabled a
 // KernelTimer hands out a pair of HIP events that the launch (through
 // hipExtLaunchKernelGGL) records at the kernel's own start and end; both

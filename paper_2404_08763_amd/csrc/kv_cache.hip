@@ -1,0 +1,141 @@
+// Quantising rows of keys and values into the cache, and reading rows back.
+//
+// Both are bound by memory at many rows and by their launch at few: a lane has 8
+// columns of one token (16 bytes of bf16, 4 of codes), four lanes share a scale,
+// and a block has consecutive rows of one head, whose records they fill or read
+// together while their lines are in the L2.  The codes come from the conversion
+// instructions: nearest value, ties to even, largest 6, scales powers of two, so
+// nothing is rounded but the value to its code.
+#include "internal.hpp"
+#include "kv4.hpp"
+
+namespace cats {
+namespace {
+
+constexpr int kThreads = 256;
+
+// Slot of a row: record and token, or false for one outside the cache.
+struct Place {
+  size_t rec;
+  int t;
+};
+template <int D> __device__ __forceinline__ bool place(const KvRowsArgs& a, int row, int head, Place& p) {
+  const int slot = a.slots[row];
+  if (slot < 0 || slot >= a.tokens) return false;
+  const int page = slot / a.page, in = slot - page * a.page;
+  p.rec = (((size_t)page * a.heads + head) * (a.page / kKvGroup) + in / kKvGroup) * kv_record_bytes(D);
+  p.t = in % kKvGroup;
+  return true;
+}
+
+// Byte of columns [8 c, 8 c + 8) of token t, values (two pieces 8 bytes apart where D is 64).
+template <int D> __device__ __forceinline__ int value_at(int t, int c) {
+  const int n = 8 * c / (D / 16), r = 8 * c % (D / 16);
+  return 8 * D + (((t >> 2) * 16 + n) * 4 + (t & 3)) * (D / 32) + r / 2;
+}
+template <int D> __device__ __forceinline__ int scale_at(bool value, int t, int blk) {
+  return 16 * D + (value ? D / 2 + ((t >> 2) * (D / 32) + blk) * 4 + (t & 3) : t * (D / 32) + blk);
+}
+
+template <int D, bool BF16> __global__ __launch_bounds__(kThreads) void k_kv_write(KvRowsArgs a) {
+  constexpr int L = D / 8;  // lanes of a row
+  const int row = blockIdx.x * (kThreads / L) + threadIdx.x / L, head = blockIdx.y, c = threadIdx.x % L;
+  const bool value = blockIdx.z != 0;
+  Place p;
+  // (all four lanes of a scale have the same row)
+  if (row >= a.rows || !place<D>(a, row, head, p)) return;
+  float f[8];
+  const size_t at = (size_t)row * (value ? a.ldv : a.ldk) + head * D + 8 * c;
+  const void* src = value ? a.v : a.k;
+  if (BF16) {
+    widen<wbf16>(*reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(src) + at), f);
+  } else {
+    const u32x4* s = reinterpret_cast<const u32x4*>(static_cast<const float*>(src) + at);
+    widen<wf32>(s[0], f);
+    widen<wf32>(s[1], f + 4);
+  }
+  uint32_t top = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(f[i]) & 0x7fffffffu);
+  top = max(top, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top, 0xb1, 0xf, 0xf, false));
+  top = max(top, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top, 0x4e, 0xf, 0xf, false));
+  const uint32_t byte = kv_scale_byte(top);
+  const float s = kv_scale(byte);
+  uint32_t w = 0;
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, f[0], f[1], s, 0);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, f[2], f[3], s, 1);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, f[4], f[5], s, 2);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, f[6], f[7], s, 3);
+  if (byte == 255u) w = 0;  // (NaN by its scale; the codes of such a block are 0)
+  uint8_t* rec = a.cache + p.rec;
+  if (!value) {
+    *reinterpret_cast<uint32_t*>(rec + p.t * (D / 2) + 4 * c) = w;
+  } else if (D == 64) {
+    uint8_t* to = rec + value_at<D>(p.t, c);
+    *reinterpret_cast<uint16_t*>(to) = (uint16_t)w;
+    *reinterpret_cast<uint16_t*>(to + 8) = (uint16_t)(w >> 16);
+  } else {
+    *reinterpret_cast<uint32_t*>(rec + value_at<D>(p.t, c)) = w;
+  }
+  if (c % 4 == 0) rec[scale_at<D>(value, p.t, c / 4)] = (uint8_t)byte;
+}
+
+template <int D, bool BF16> __global__ __launch_bounds__(kThreads) void k_kv_read(KvRowsArgs a) {
+  constexpr int L = D / 8;
+  const int row = blockIdx.x * (kThreads / L) + threadIdx.x / L, head = blockIdx.y, c = threadIdx.x % L;
+  const bool value = blockIdx.z != 0;
+  Place p;
+  if (row >= a.rows || !place<D>(a, row, head, p)) return;
+  const uint8_t* rec = a.cache + p.rec;
+  uint32_t w;
+  if (!value) {
+    w = *reinterpret_cast<const uint32_t*>(rec + p.t * (D / 2) + 4 * c);
+  } else if (D == 64) {
+    const uint8_t* from = rec + value_at<D>(p.t, c);
+    w = *reinterpret_cast<const uint16_t*>(from) | (uint32_t)*reinterpret_cast<const uint16_t*>(from + 8) << 16;
+  } else {
+    w = *reinterpret_cast<const uint32_t*>(rec + value_at<D>(p.t, c));
+  }
+  const float s = kv_scale(rec[scale_at<D>(value, p.t, c / 4)]);
+  void* dst = value ? a.v_out : a.k_out;
+  const size_t at = ((size_t)row * a.heads + head) * D + 8 * c;
+  if (BF16) {
+    u32x4 o;
+    o.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 0));
+    o.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 1));
+    o.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 2));
+    o.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 3));
+    *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(dst) + at) = o;
+  } else {
+    const f32x2 v0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, s, 0);
+    const f32x2 v1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, s, 1);
+    const f32x2 v2 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, s, 2);
+    const f32x2 v3 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, s, 3);
+    f32x4* o = reinterpret_cast<f32x4*>(static_cast<float*>(dst) + at);
+    o[0] = f32x4{v0[0], v0[1], v1[0], v1[1]};
+    o[1] = f32x4{v2[0], v2[1], v3[0], v3[1]};
+  }
+}
+
+template <int D> hipError_t go(bool write, bool bf16, const KvRowsArgs& a, hipStream_t s) {
+  const dim3 grid((a.rows + kThreads / (D / 8) - 1) / (kThreads / (D / 8)), a.heads, 2);
+  KernelTimer tm(write ? "kv_write" : "kv_read", s);
+#define CATS_GO(K) hipExtLaunchKernelGGL((K), grid, dim3(kThreads), 0, s, tm.start(), tm.stop(), 0, a)
+  if (write) {
+    if (bf16) CATS_GO((k_kv_write<D, true>));
+    else CATS_GO((k_kv_write<D, false>));
+  } else {
+    if (bf16) CATS_GO((k_kv_read<D, true>));
+    else CATS_GO((k_kv_read<D, false>));
+  }
+#undef CATS_GO
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_kv_rows(bool write, bool bf16, int d, const KvRowsArgs& a, hipStream_t s) {
+  return d == 64 ? go<64>(write, bf16, a, s) : d == 128 ? go<128>(write, bf16, a, s) : go<256>(write, bf16, a, s);
+}
+
+}  // namespace cats

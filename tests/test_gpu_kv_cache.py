@@ -1,0 +1,146 @@
+"""Rows written to the cache in 4 bits and read back: equal to the format's reference bit for bit."""
+import pytest
+import torch
+
+import paper_2404_08763_amd as P
+
+from gpu_util import say
+from kv_util import BF16, F32, garbage, gen, held, put
+
+pytestmark = pytest.mark.gpu
+IDS = {F32: "f32", BF16: "bf16"}
+
+
+def _rows(n, heads, d, dtype, seed):
+    g = gen(seed)
+    x = torch.randn((n, heads, d), generator=g) * torch.exp(2 * torch.randn((n, heads, 1), generator=g))
+    x[..., 0] = torch.round(4 * x[..., 0]) / 4  # ties among them
+    return x.to(dtype)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=IDS.get)
+@pytest.mark.parametrize("n,heads,d,page", [(1, 1, 64, 16), (1, 40, 128, 64), (37, 3, 64, 48), (33, 2, 256, 32),
+                                            (70, 5, 128, 16), (300, 8, 128, 256)])
+def test_write_and_read(n, heads, d, page, dtype):
+    say("kv rows", n, heads, d, page, dtype)
+    pages = (2 * n + page - 1) // page + 1
+    cpu = garbage(pages, heads, d, page)
+    cache = cpu.cuda()
+    k, v = _rows(n, heads, d, dtype, 1), _rows(n, heads, d, dtype, 2)
+    slots = torch.randperm(pages * page, generator=gen(3))[:n].to(torch.int32)
+    P.kv_write(cache, k.cuda(), v.cuda(), slots.cuda())
+    put(cpu, slots, k, v)
+    assert torch.equal(cache.cpu(), cpu)  # every byte, those of no row as they were
+    for out in (F32, BF16):
+        rk, rv = P.kv_read(cache, slots.cuda(), dtype=out)
+        assert torch.equal(rk.cpu().double(), held(k)) and torch.equal(rv.cpu().double(), held(v))
+
+
+def test_special_values():
+    """Zeros, infinities, NaN, the smallest and largest magnitudes; a block's neighbours keep theirs."""
+    d = 128
+    x = _rows(12, 2, d, F32, 5)
+    x[0, 0, :32] = 0.0
+    x[1, 0, 5], x[2, 1, 40], x[3, 0, 127] = float("nan"), float("inf"), float("-inf")
+    x[4, 1, 64:96] *= 1e-40
+    x[5, 0, 3], x[6, 1, 33] = 3.4e38, -2.6e38
+    x[7] *= 2.0 ** -120
+    x[8, 0, :32] = 0.0
+    x[8, 0, 7] = -1e-45
+    say("kv special values")
+    cpu = garbage(1, 2, d, 16)
+    cache = cpu.cuda()
+    slots = torch.arange(12, dtype=torch.int32)
+    P.kv_write(cache, x.cuda(), x.flip(0).contiguous().cuda(), slots.cuda())
+    put(cpu, slots, x, x.flip(0))
+    assert torch.equal(cache.cpu(), cpu)
+    rk, rv = P.kv_read(cache, slots.cuda(), dtype=F32)
+    for got, want in ((rk, held(x)), (rv, held(x.flip(0)))):
+        assert torch.equal(got.cpu().double().nan_to_num(nan=7e77), want.nan_to_num(nan=7e77))
+    assert torch.isnan(held(x)[1, 0, :32]).all() and not torch.isnan(held(x)[1, 0, 32:]).any()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=IDS.get)
+def test_strided_rows_and_padding(dtype):
+    """Keys and values as columns of a projection's rows; rows with slots outside the cache
+    are left out of the cache, and of what is read."""
+    n, heads, d, page = 21, 4, 64, 32
+    say("kv strided", dtype)
+    qkv = torch.randn((n, 5 * heads * d + 8), generator=gen(7)).to(dtype)
+    k, v = qkv[:, heads * d:2 * heads * d], qkv[:, 3 * heads * d:4 * heads * d]
+    slots = torch.randperm(3 * page, generator=gen(8))[:n].to(torch.int32)
+    slots[[0, 5, 9, 20]] = torch.tensor([-1, 3 * page, 2 ** 31 - 1, -2 ** 31], dtype=torch.int32)
+    cpu = garbage(3, heads, d, page)
+    cache, dev = cpu.cuda(), qkv.cuda()
+    P.kv_write(cache, dev[:, heads * d:2 * heads * d], dev[:, 3 * heads * d:4 * heads * d].unflatten(1, (heads, d)),
+               slots.cuda())
+    put(cpu, slots, k.unflatten(1, (heads, d)), v.unflatten(1, (heads, d)))
+    assert torch.equal(cache.cpu(), cpu)
+    out = tuple(torch.full((n, heads, d), 3.0, device="cuda", dtype=dtype) for _ in range(2))
+    rk, rv = P.kv_read(cache, slots.cuda(), out=out)
+    outside = [0, 5, 9, 20]
+    inside = [i for i in range(n) if i not in outside]
+    assert (rk[outside] == 3).all() and (rv[outside] == 3).all()
+    assert torch.equal(rk[inside].cpu().double(), held(k.unflatten(1, (heads, d))[inside]))
+    assert torch.equal(rv[inside].cpu().double(), held(v.unflatten(1, (heads, d))[inside]))
+
+
+def test_one_row_of_any_stride():
+    """A single row's stride is no pitch."""
+    say("kv one row")
+    x = torch.randn((1, 128), generator=gen(9)).cuda().as_strided((1, 128), (3, 1))
+    cache = P.kv_cache(1, 2, 64, page=16)
+    P.kv_write(cache, x, x, torch.tensor([4], dtype=torch.int32, device="cuda"))
+    rk, rv = P.kv_read(cache, torch.tensor([4], dtype=torch.int32, device="cuda"), dtype=F32)
+    want = held(x.cpu().view(1, 2, 64))
+    assert torch.equal(rk.cpu().double(), want) and torch.equal(rv.cpu().double(), want)
+
+
+def test_cache_beyond_32_bits():
+    """Offsets past 2^32 bytes: a page at the end of a cache of 4.6 GiB."""
+    say("kv far pages")
+    pages, heads, d, page = 17700, 8, 128, 256
+    cache = P.kv_cache(pages, heads, d, page=page)
+    assert cache.numel() > 4.5 * 2 ** 30
+    k, v = _rows(40, heads, d, BF16, 11), _rows(40, heads, d, BF16, 12)
+    slots = torch.arange(pages * page - 40, pages * page, dtype=torch.int32)
+    low = torch.arange(40, dtype=torch.int32)
+    P.kv_write(cache, v.cuda(), k.cuda(), low.cuda())
+    P.kv_write(cache, k.cuda(), v.cuda(), slots.cuda())
+    rk, rv = P.kv_read(cache, slots.cuda())
+    assert torch.equal(rk.cpu().double(), held(k)) and torch.equal(rv.cpu().double(), held(v))
+    rk, rv = P.kv_read(cache, low.cuda())
+    assert torch.equal(rk.cpu().double(), held(v)) and torch.equal(rv.cpu().double(), held(k))
+
+
+def test_graph_and_streams():
+    """Captured once, replayed on other rows and slots; and on a stream of the caller's."""
+    n, heads, d, page = 9, 2, 128, 16
+    say("kv graph")
+    cache = garbage(4, heads, d, page).cuda()
+    k, v = (torch.zeros((n, heads, d), device="cuda", dtype=BF16) for _ in range(2))
+    slots = torch.arange(n, dtype=torch.int32, device="cuda")
+    out = tuple(torch.zeros((n, heads, d), device="cuda") for _ in range(2))
+    P.kv_write(cache, k, v, slots)
+    P.kv_read(cache, slots, out=out)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        P.kv_write(cache, k, v, slots)
+        P.kv_read(cache, slots, out=out)
+    for r in range(3):
+        a, b = _rows(n, heads, d, BF16, 20 + r), _rows(n, heads, d, BF16, 30 + r)
+        k.copy_(a)
+        v.copy_(b)
+        slots.copy_(torch.randperm(4 * page, generator=gen(r))[:n])
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out[0].cpu().double(), held(a)) and torch.equal(out[1].cpu().double(), held(b))
+        _ = (k.float() * 2).sum()
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        P.kv_write(cache, v, k, slots)
+        rk, rv = P.kv_read(cache, slots)
+    s.synchronize()
+    assert torch.equal(rk.cpu().double(), held(b)) and torch.equal(rv.cpu().double(), held(a))
