@@ -512,8 +512,8 @@ cats_status cats_kv_read(const cats_kv_cache* cache, const int32_t* slots, int32
  * left as they were.  A row that sees a token of a page outside [0, pages) becomes NaN.
  * Masked tokens have no effect, whatever the cache holds for them.
  * Products of q and the cache's values are exact and summed in fp32, as is the
- * softmax; its weights enter the second product with 16 bits for bf16 rows and
- * 24 for fp32 rows.  A row's bits may depend on the other sequences of the
+ * softmax; its weights enter the second product rounded to f16 (11 bits) for bf16
+ * rows, as two such parts (22 bits) for fp32 rows.  A row's bits may depend on the other sequences of the
  * call (how the keys are shared out), but not from run to run.
  * Workspace: cats_kv_attention_workspace_bytes(N, B, hq, heads, d), which serves
  * every call of up to as many rows and sequences of the same heads.

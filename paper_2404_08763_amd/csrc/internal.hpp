@@ -323,9 +323,9 @@ struct KvAttentionArgs {
   int tiles;             // without a plan: tiles of a sequence's query heads
   int blocks;
   // workspace
-  int* head;             // plan: tiles, units of a head
+  int* head;             // plan: tiles of a head, and what they cost
   KvPlanEntry* plan;
-  int* prefix;           // units in front of each tile
+  int* prefix;           // what is in front of each tile (KvRun)
   int* first;            // [B + 1] first tile of each sequence
   int4* desc;            // [blocks] the sum that begins in each block
   float* part;           // [blocks x 2] partial sums
@@ -333,6 +333,8 @@ struct KvAttentionArgs {
 // Workspace of a call, and at most of any call of up to N rows and B sequences.
 size_t kv_attention_bytes(int N, int B, int hq, int hkv, int d, bool bf16, bool planned);
 size_t kv_attention_most(int N, int B, int hq, int hkv, int d);
+// Whether the call's work can be counted in 32 bits (a's sizes and limit).
+bool kv_attention_fits(const KvAttentionArgs& a, int d, bool bf16);
 hipError_t launch_kv_attention(KvAttentionArgs a, int d, bool bf16, hipStream_t s);
 
 // Optional per-kernel timing (cats_timer_*): while the timer is enabled a

@@ -248,6 +248,8 @@ cats_status cats_kv_attention(const void* q, int32_t dtype, int32_t N, int32_t h
   a.c = scale * 1.44269504088896340736f;
   a.window = window;
   a.head = static_cast<int*>(ws);
+  if (!cats::kv_attention_fits(a, cache->d, dtype == CATS_BF16))
+    return fail(CATS_ERR_SHAPE, "%d rows of %d sequences over tables of %d tokens are too many for one call", (int)N, (int)B, a.limit);
   return launched(cats::launch_kv_attention(a, cache->d, dtype == CATS_BF16, static_cast<hipStream_t>(stream)), stream,
                   "cats_kv_attention");
 }

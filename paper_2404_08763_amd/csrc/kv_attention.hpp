@@ -1,0 +1,585 @@
+// What the attention kernels over the cache in 4 bits share: the keys a tile of rows reads,
+// how the blocks share the work, the operands of the matrix products.
+#pragma once
+
+#include "internal.hpp"
+#include "kv4.hpp"
+
+namespace cats {
+
+constexpr int kKvThreads = 256, kKvWaves = 4;
+constexpr float kLow = -3.402823466e+38f;  // maximum of a row that has seen no key
+// A row's exponents are counted from its maximum less kLead, which is moved only when a
+// score is kLazy above that, so that O is rarely multiplied: p is 2^15 at most, and f16's
+// least number 2^-31 of the largest.
+constexpr float kLead = 7.f, kLazy = 8.f;
+
+
+// ---- the work of a call -------------------------------------------------------------
+
+__device__ __forceinline__ int kv_length(const KvAttentionArgs& a, int b) { return min(max(a.lens[b], 0), a.limit); }
+
+// Queries [start, start + nq) of a sequence, whatever q_start holds.
+__device__ __forceinline__ int kv_queries(const KvAttentionArgs& a, int b, int& start) {
+  if (!a.q_start) {
+    start = b;
+    return 1;
+  }
+  start = min(max(a.q_start[b], 0), a.N);
+  return max(min(max(a.q_start[b + 1], 0), a.N) - start, 0);
+}
+
+// A tile: rows [row0, row0 + rows) of a sequence, counted over its queries and a key head's
+// query heads, and the keys [lo, hi) it reads, from the record of lo on, in units of UNIT tokens.
+struct KvTile {
+  int b, row0, rows, start, nq, len;
+  int first, last;  // positions of its first and last row
+  int lo, hi, units;
+};
+template <int UNIT> __device__ __forceinline__ void kv_span(const KvAttentionArgs& a, int G, KvTile& t) {
+  t.first = t.len - t.nq + t.row0 / G;
+  t.last = t.len - t.nq + (t.row0 + t.rows - 1) / G;
+  t.hi = min(max(t.last + 1, 0), t.len);
+  t.lo = a.window > 0 ? min(max(t.first - a.window + 1, 0), t.hi) : 0;
+  t.lo &= ~(kKvGroup - 1);
+  t.units = max(1, (t.hi - t.lo + UNIT - 1) / UNIT);
+}
+template <int UNIT> __device__ __forceinline__ KvTile kv_tile(const KvAttentionArgs& a, int G, int b, int row0, int R) {
+  KvTile t;
+  t.b = b;
+  t.row0 = row0;
+  t.nq = kv_queries(a, b, t.start);
+  t.rows = min(R, t.nq * G - row0);
+  t.len = kv_length(a, b);
+  kv_span<UNIT>(a, G, t);
+  return t;
+}
+
+// Inclusive prefix over a wave.
+__device__ __forceinline__ int wave_prefix(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);  // row_shr 1, 2, 4, 8
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);  // row_bcast 15 into rows 1 and 3
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);  // row_bcast 31 into rows 2 and 3
+  return x;
+}
+
+// Exclusive prefix of v over the block's threads and its total.
+template <int THREADS> __device__ __forceinline__ int block_prefix(int v, int& total, int* sh) {
+  const int w = threadIdx.x / 64, x = wave_prefix(v);
+  __syncthreads();
+  if (threadIdx.x % 64 == 63) sh[w] = x;
+  __syncthreads();
+  int before = 0;
+  total = 0;
+#pragma unroll
+  for (int i = 0; i < THREADS / 64; ++i) {
+    if (i < w) before += sh[i];
+    total += sh[i];
+  }
+  total = (int)uniform_u32(total);
+  return before + x - v;
+}
+
+// n / d for a quotient below 2^32.
+__device__ __forceinline__ uint32_t quotient(uint64_t n, uint32_t d) {
+  return (n >> 32) == 0 ? (uint32_t)n / d : (uint32_t)(n / d);
+}
+
+// A block's share.  The tiles of a head lie one behind the other, the heads behind each other,
+// each tile as its units and LEAD more, which stand for what a tile costs besides; each
+// block has a run of that line, all of one length but for one, whatever the sequences' lengths.
+// Runs next to each other are on one XCD, which shares their keys.  A tile's parts are in
+// consecutive blocks: none is empty but those behind the last.
+struct KvRun {
+  int lb;              // the block's place on the line
+  uint32_t base, rem;  // length of a run, and how many are one longer
+  uint64_t p, p1;      // the run
+  int tiles;           // of a head, or (no plan) of a sequence
+  int h, e, b, skip;   // head, tile (no plan: of sequence b), and where in the tile
+};
+
+template <bool PLAN, int UNIT, int LEAD, int R>
+__device__ __forceinline__ bool kv_run(const KvAttentionArgs& a, KvRun& r, int* sh) {
+  const int G = a.hq / a.hkv;
+  r.tiles = PLAN ? a.head[0] : a.tiles;
+  const auto cost = [&](int b) { return b < a.B ? r.tiles * (kv_tile<UNIT>(a, G, b, 0, R).units + LEAD) : 0; };
+  uint32_t W = 0;  // of a head
+  int mine = 0, before = 0;
+  if constexpr (PLAN) {
+    W = (uint32_t)a.head[1];
+  } else {
+    for (int base = 0; base < a.B; base += kKvThreads) {
+      int total;
+      mine = cost(base + threadIdx.x);
+      before = block_prefix<kKvThreads>(mine, total, sh);
+      W += (uint32_t)total;
+    }
+  }
+  const uint64_t T = (uint64_t)W * (uint32_t)a.hkv;
+  const uint32_t nb = T < (uint32_t)a.blocks ? (uint32_t)T : (uint32_t)a.blocks;
+  r.lb = nb < (uint32_t)a.blocks ? (int)blockIdx.x : (int)((blockIdx.x % 8) * (nb / 8) + blockIdx.x / 8);
+  if (threadIdx.x == 0) a.desc[r.lb] = int4{0, 0, 0, 0};
+  if ((uint32_t)r.lb >= nb) return false;
+  r.base = quotient(T, nb);
+  r.rem = (uint32_t)(T - (uint64_t)r.base * nb);
+  r.p = (uint64_t)r.lb * r.base + min((uint32_t)r.lb, r.rem);
+  r.p1 = r.p + r.base + ((uint32_t)r.lb < r.rem ? 1 : 0);
+  r.h = (int)quotient(r.p, W);
+  const uint32_t x = (uint32_t)(r.p - (uint64_t)(uint32_t)r.h * W);
+  if constexpr (PLAN) {
+    int lo = 0, n = r.tiles;  // the last tile whose prefix is not behind x
+    while (n > 1) {
+      const int stride = (n + kKvThreads - 1) / kKvThreads, at = threadIdx.x * stride;
+      const int last = (int)uniform_u32(__syncthreads_count(at < n && (uint32_t)a.prefix[lo + at] <= x)) - 1;
+      lo += last * stride;
+      n = min(stride, n - last * stride);
+    }
+    r.e = lo;
+    r.b = 0;
+    r.skip = (int)(x - (uint32_t)a.prefix[lo]);
+  } else {
+    uint32_t sum = 0;
+    for (int base = 0;; base += kKvThreads) {
+      int total = 0;
+      if (a.B > kKvThreads) {  // (else as it was counted above)
+        mine = cost(base + threadIdx.x);
+        before = block_prefix<kKvThreads>(mine, total, sh);
+      }
+      const uint32_t at = sum + (uint32_t)before;
+      if (at <= x && x < at + (uint32_t)mine) {
+        sh[4] = base + threadIdx.x;
+        sh[5] = (int)(x - at);
+        sh[6] = mine;
+      }
+      sum += (uint32_t)total;
+      if (a.B <= kKvThreads || x < sum) break;
+    }
+    __syncthreads();
+    r.b = (int)uniform_u32(sh[4]);
+    const uint32_t in = uniform_u32(sh[5]), one = uniform_u32(sh[6]) / r.tiles;
+    r.e = (int)(in / one);
+    r.skip = (int)(in - r.e * one);
+  }
+  r.h = (int)uniform_u32(r.h);
+  r.skip = (int)uniform_u32(r.skip);
+  return true;
+}
+
+// The run's present tile.
+template <bool PLAN, int UNIT, int R> __device__ __forceinline__ KvTile kv_tile_of(const KvAttentionArgs& a, int G, const KvRun& r) {
+  if constexpr (PLAN) {
+    const KvPlanEntry t = a.plan[r.e];
+    return kv_tile<UNIT>(a, G, (int)uniform_u32(t.b), (int)uniform_u32(t.row0), R);
+  } else {
+    return kv_tile<UNIT>(a, G, r.b, r.e * R, R);
+  }
+}
+
+// The part of the tile that is in the run: units [u0, u1), possibly none.
+struct KvPart {
+  int u0, u1;
+  bool head, whole;  // begins the tile; is all of it
+};
+template <int LEAD> __device__ __forceinline__ KvPart kv_part(const KvRun& r, const KvTile& t) {
+  const uint64_t left = r.p1 - r.p;
+  const int all = t.units + LEAD, c1 = left < (uint64_t)(all - r.skip) ? r.skip + (int)left : all;
+  KvPart p;
+  p.u0 = max(0, r.skip - LEAD);
+  p.u1 = max(0, c1 - LEAD);
+  p.head = r.skip <= LEAD && p.u1 > 0;
+  p.whole = p.head && c1 == all;
+  return p;
+}
+
+// Notes a sum that begins in this block and ends in a later one, and goes on to the next tile.
+template <bool PLAN, int LEAD>
+__device__ __forceinline__ void kv_next(const KvAttentionArgs& a, KvRun& r, const KvTile& t, const KvPart& p) {
+  const uint64_t end = r.p - (uint32_t)r.skip + (uint32_t)(t.units + LEAD);  // of the tile, on the line
+  if (p.head && !p.whole && threadIdx.x == 0) {
+    const uint64_t x = end - 1, big = (uint64_t)r.rem * (r.base + 1);
+    const uint32_t until = x < big ? quotient(x, r.base + 1) : r.rem + quotient(x - big, r.base);
+    a.desc[r.lb] = int4{(int)until - r.lb + 1, r.h, t.b, t.row0};
+  }
+  r.p = end < r.p1 ? end : r.p1;
+  r.skip = 0;
+  ++r.e;
+  if constexpr (PLAN) {
+    if (r.e == r.tiles) r.e = 0, ++r.h;
+  } else {
+    if (r.e == r.tiles) {
+      r.e = 0;
+      if (++r.b == a.B) r.b = 0, ++r.h;
+    }
+  }
+}
+
+// ---- the cache's records ----------------------------------------------------------------
+
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+
+// Words that no kernel of the call writes, at an address equal on all lanes: a scalar load.
+__device__ __forceinline__ int scalar_load(const int* p, size_t i) {
+  return reinterpret_cast<const __attribute__((address_space(4))) int*>(reinterpret_cast<uintptr_t>(p))[i];
+}
+
+// The lane's parts of a record (kv4.hpp).
+template <int D> struct KvLane {
+  uint32_t k, v, ks, vs;
+  __device__ __forceinline__ KvLane() {
+    const uint32_t lane = threadIdx.x % 64, m = lane % 16, g = lane / 16;
+    k = m * (D / 2) + g * (D / 8);
+    v = 8 * D + lane * (D / 8);
+    ks = 16 * D + m * (D / 32) + (D == 256 ? 2 * g : D == 128 ? g : g / 2);
+    vs = 16 * D + D / 2 + g * (D / 8) + m * D / 512 * 4;
+  }
+};
+
+// The records of a key head of a sequence.
+template <int D> struct KvRecords {
+  const int* table;
+  const uint8_t* base;
+  uint32_t stride, most, magic, groups, pages;
+  __device__ __forceinline__ KvRecords(const KvAttentionArgs& a, int b, int h, int hi) {
+    table = a.table + (size_t)b * a.width;
+    base = a.cache + (size_t)h * a.groups * kv_record_bytes(D);
+    stride = (uint32_t)(a.hkv * a.groups) * kv_record_bytes(D);
+    most = (uint32_t)(max(hi, 1) - 1) / kKvGroup;  // the last record some row sees
+    magic = a.magic;
+    groups = (uint32_t)a.groups;
+    pages = (uint32_t)a.pages;
+  }
+  // A record's page and its place there; what is behind the last one is that once more.
+  struct Place {
+    uint32_t page, in;
+  };
+  __device__ __forceinline__ Place find(uint32_t rec) const {
+    rec = min(rec, most);
+    const uint32_t at = __umulhi(rec << 1, magic);
+    return Place{(uint32_t)scalar_load(table, at), (rec - at * groups) * kv_record_bytes(D)};
+  }
+  // All ones where the page is none of the cache's (whose first page is read for it).
+  __device__ __forceinline__ uint32_t bad(const Place& p) const { return p.page < pages ? 0u : 0xffffu; }
+  __device__ __forceinline__ __amdgpu_buffer_rsrc_t at(const Place& p) const {
+    return make_rsrc(base + (uint64_t)(p.page < pages ? p.page : 0u) * stride + p.in, kv_record_bytes(D));
+  }
+};
+
+// The lane's words at an offset in a record, whose address is equal on all lanes: a buffer
+// load adds the two (and reads nothing behind the record).
+// ONCE: for no later reader (non-temporal).
+template <int W, bool ONCE>
+__device__ __forceinline__ void load_words(__amdgpu_buffer_rsrc_t record, uint32_t off, uint32_t* w) {
+  if constexpr (W == 2) {
+    const auto v = __builtin_amdgcn_raw_buffer_load_b64(record, (int)off, 0, ONCE ? 2 : 0);
+    w[0] = v[0];
+    w[1] = v[1];
+  } else {
+#pragma unroll
+    for (int i = 0; i < W / 4; ++i) {
+      const u32x4 v = ONCE ? ld_buf16_stream(record, off + 16 * i) : ld_buf16(record, off + 16 * i);
+      w[4 * i] = v.x;
+      w[4 * i + 1] = v.y;
+      w[4 * i + 2] = v.z;
+      w[4 * i + 3] = v.w;
+    }
+  }
+}
+
+// The scales of a lane's keys: one, or two of 256 columns.
+template <int D> __device__ __forceinline__ uint32_t load_key_scales(__amdgpu_buffer_rsrc_t record, uint32_t off) {
+  if constexpr (D == 256) return (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(record, (int)off, 0, 0);
+  else return (uint8_t)__builtin_amdgcn_raw_buffer_load_b8(record, (int)off, 0, 0);
+}
+
+template <typename T> __device__ __forceinline__ T as_eight(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  const u32x4 v = {a, b, c, d};
+  return __builtin_bit_cast(T, v);
+}
+
+// The two values of byte SEL, as bf16 (exact for every scale) or f16 (exact where kNarrow says so).
+template <int SEL> __device__ __forceinline__ uint32_t two_bf16(uint32_t w, float s) {
+  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, SEL));
+}
+template <int SEL> __device__ __forceinline__ uint32_t two_f16(uint32_t w, float s) {
+  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, s, SEL));
+}
+__device__ __forceinline__ bf16x8 eight_of(uint32_t w, float s) {
+  return as_eight<bf16x8>(two_bf16<0>(w, s), two_bf16<1>(w, s), two_bf16<2>(w, s), two_bf16<3>(w, s));
+}
+// Byte C of the lane's D / 32 bytes of token i.
+template <int D, int C, bool F16> __device__ __forceinline__ uint32_t value_pair(const uint32_t* v, int i, float s) {
+  if constexpr (D == 64) {
+    if (F16) return i % 2 ? two_f16<2 + C>(v[i / 2], s) : two_f16<C>(v[i / 2], s);
+    return i % 2 ? two_bf16<2 + C>(v[i / 2], s) : two_bf16<C>(v[i / 2], s);
+  } else {
+    const uint32_t w = v[i * (D / 128) + C / 4];
+    return F16 ? two_f16<C % 4>(w, s) : two_bf16<C % 4>(w, s);
+  }
+}
+
+__device__ __forceinline__ uint32_t low_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x05040100u); }
+__device__ __forceinline__ uint32_t high_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); }
+
+// V^T's operands of columns 2 C and 2 C + 1 (of each lane's D / 16): the tokens of two records side by side.
+template <int D, int C, bool F16, typename T>
+__device__ __forceinline__ void value_operands(const uint32_t (&v)[2][D / 32], const float (&sc)[2][4], T (&out)[2]) {
+  uint32_t e[2][4];
+#pragma unroll
+  for (int u = 0; u < 2; ++u)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) e[u][i] = value_pair<D, C, F16>(v[u], i, sc[u][i]);
+  out[0] = as_eight<T>(low_halves(e[0][0], e[0][1]), low_halves(e[0][2], e[0][3]), low_halves(e[1][0], e[1][1]),
+                       low_halves(e[1][2], e[1][3]));
+  out[1] = as_eight<T>(high_halves(e[0][0], e[0][1]), high_halves(e[0][2], e[0][3]), high_halves(e[1][0], e[1][1]),
+                       high_halves(e[1][2], e[1][3]));
+}
+// Whether a value scale's byte is outside [109, 140], 2^-18 to 2^13, for which f16 has all
+// of the codes' values: bits of the four bytes that say so.  (The sum of a byte above
+// 236 carries into the next, but is itself outside.)
+__device__ __forceinline__ uint32_t not_narrow(uint32_t vs) { return ((vs + 0x13131313u) ^ 0x80808080u) & 0xe0e0e0e0u; }
+
+// Codes of 0 with scales of 1.
+template <int W> __device__ __forceinline__ void no_values(uint32_t (&v)[W], uint32_t& vs) {
+#pragma unroll
+  for (int i = 0; i < W; ++i) v[i] = 0u;
+  vs = 0x7f7f7f7fu;
+}
+
+// f as three bf16 parts, all 24 bits of it.
+__device__ __forceinline__ float cut(float f) { return __uint_as_float(__float_as_uint(f) & 0xffff0000u); }
+__device__ __forceinline__ void split8(const float* f, bf16x8* out) {
+  float r[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) r[i] = f[i];
+#pragma unroll
+  for (int p = 0; p < 3; ++p) {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = high_halves(__float_as_uint(r[2 * i]), __float_as_uint(r[2 * i + 1]));
+    out[p] = as_eight<bf16x8>(w[0], w[1], w[2], w[3]);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) r[i] -= cut(r[i]);
+  }
+}
+
+__device__ __forceinline__ bool sees(const KvAttentionArgs& a, int pos, int j) {
+  return j <= pos && (a.window <= 0 || j > pos - a.window);
+}
+
+template <bool BF16> __device__ __forceinline__ void store_out(void* out, size_t at, const f32x4& v) {
+  if (BF16) {
+    typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+    *reinterpret_cast<bf16x4*>(static_cast<uint16_t*>(out) + at) = bf16x4{(__bf16)v[0], (__bf16)v[1], (__bf16)v[2], (__bf16)v[3]};
+  } else {
+    *reinterpret_cast<f32x4*>(static_cast<float*>(out) + at) = v;
+  }
+}
+
+// Eight columns of a row of q as bf16 parts.
+template <int NQ> __device__ __forceinline__ void load_q8(const void* q, size_t at, bf16x8* out) {
+  if constexpr (NQ == 1) {
+    out[0] = *reinterpret_cast<const bf16x8*>(static_cast<const uint16_t*>(q) + at);
+  } else {
+    const f32x4* p = reinterpret_cast<const f32x4*>(static_cast<const float*>(q) + at);
+    const f32x4 x = p[0], y = p[1];
+    const float f[8] = {x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
+    split8(f, out);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      // an infinity or NaN is in the first part alone
+      const bool whole = (__float_as_uint(f[e]) & 0x7f800000u) == 0x7f800000u;
+      out[0][e] = whole ? (__bf16)f[e] : out[0][e];
+      out[1][e] = whole ? (__bf16)0.f : out[1][e];
+      out[2][e] = whole ? (__bf16)0.f : out[2][e];
+    }
+  }
+}
+
+// ---- a step ----------------------------------------------------------------------------------
+
+// A wave's rows, QT tiles of 16, one to a lane of 16: their sums.
+template <int D, int QT> struct KvSums {
+  f32x4 o[QT][D / 16];  // o[t][j][i]: row lane % 16, column g D/4 + i D/16 + j
+  float m[QT], l[QT];   // what the exponents are counted from, the lane's part of the sum
+  int pos[QT];          // the row's position, -1 and less: sees nothing
+};
+
+// The softmax of a step: scores z of the tokens [tok, tok + 32) become weights, the sums
+// what they are counted from.  `masked`: not every row sees all of the tokens.
+template <int D, int QT>
+__device__ __forceinline__ void weights(KvSums<D, QT>& w, const KvAttentionArgs& a, f32x4 (&z)[QT][2], int tok, bool masked) {
+  const int g = threadIdx.x % 64 / 16;
+  if (__builtin_expect(masked, 0)) {
+    asm volatile("");  // (a branch: these cost a step a third more where no row needs them)
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int t = 0; t < QT; ++t)
+          z[t][u][i] = sees(a, w.pos[t], tok + 16 * u + 4 * g + i) ? z[t][u][i] : -__builtin_inff();
+  }
+  float top[QT];
+  bool rise = false;
+#pragma unroll
+  for (int t = 0; t < QT; ++t) {
+    top[t] = z[t][0][0];
+#pragma unroll
+    for (int i = 1; i < 8; ++i) top[t] = fmaxf(top[t], z[t][i / 4][i % 4]);
+    top[t] *= a.c;
+    rise |= top[t] > w.m[t] + (kLead + kLazy);  // (kLow plus that is kLow)
+  }
+  if (__builtin_expect(__ballot(rise) != 0, 0)) {
+    asm volatile("");
+#pragma unroll
+    for (int t = 0; t < QT; ++t) {
+      float x = fmaxf(top[t], __shfl_xor(top[t], 16));
+      x = fmaxf(x, __shfl_xor(x, 32));
+      const float m = fmaxf(w.m[t], x - kLead), f = __builtin_amdgcn_exp2f(w.m[t] - m);
+      w.m[t] = m;
+      w.l[t] *= f;
+#pragma unroll
+      for (int j = 0; j < D / 16; ++j) w.o[t][j] *= f;
+    }
+  }
+#pragma unroll
+  for (int t = 0; t < QT; ++t) {
+    float l = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      z[t][i / 4][i % 4] = __builtin_amdgcn_exp2f(fmaf(z[t][i / 4][i % 4], a.c, -w.m[t]));
+      l += z[t][i / 4][i % 4];
+    }
+    w.l[t] += l;
+  }
+}
+
+// The weights as NP f16 parts, the second product's operands.
+template <int QT, int NP> __device__ __forceinline__ void weight_operands(const f32x4 (&z)[QT][2], f16x8 (&part)[QT][NP]) {
+#pragma unroll
+  for (int t = 0; t < QT; ++t)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      float r = z[t][i / 4][i % 4];
+#pragma unroll
+      for (int n = 0; n < NP; ++n) {
+        part[t][n][i] = (_Float16)r;
+        r -= (float)part[t][n][i];
+      }
+    }
+}
+
+// The value scales of tokens from `hi` on, of which no row sees any, as 1: a hidden token's
+// weight is 0, but 0 times an infinity or NaN is not.  first: of the lane's four.
+__device__ __forceinline__ uint32_t hidden_as_one(uint32_t vs, int first, int hi) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (first + i >= hi) vs = (vs & ~(0xffu << (8 * i))) | 0x7fu << (8 * i);
+  return vs;
+}
+
+template <int D, int C, int QT>
+__device__ __forceinline__ void wide_products(KvSums<D, QT>& w, const uint32_t (&v)[2][D / 32], const float (&sc)[2][4],
+                                              const bf16x8 (&part)[QT][3]) {
+  bf16x8 f[2];
+  value_operands<D, C, false>(v, sc, f);
+#pragma unroll
+  for (int t = 0; t < QT; ++t)
+#pragma unroll
+    for (int n = 2; n >= 0; --n)
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+        w.o[t][2 * C + j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f[j], part[t][n], w.o[t][2 * C + j], 0, 0, 0);
+  if constexpr (C + 1 < D / 32) wide_products<D, C + 1, QT>(w, v, sc, part);
+}
+
+// The second product where a value scale is outside f16's range or NaN: bf16 values, whose
+// range is the scales', and P in three bf16 parts.  A hidden token's p is 0, but 0 times NaN
+// is not: scales of NaN (and the two whose values leave fp32, which are in a cache only
+// where nothing was written) become 1, and the rows that see such a token NaN in its columns.
+// The product of f16 operands follows in every step, here with values of 0 (no_values): where
+// it followed in other steps alone, every step copied the sums.
+template <int D, int QT>
+__device__ __forceinline__ void wide_values(KvSums<D, QT>& w, const KvAttentionArgs& a, const uint32_t (&v)[2][D / 32],
+                                         const uint32_t (&scales)[2], const f32x4 (&p)[QT][2], int tok) {
+  const int lane = threadIdx.x % 64, g = lane / 16;
+  uint32_t odd = 0, vs[2] = {scales[0], scales[1]};
+  float sc[2][4];
+#pragma unroll
+  for (int u = 0; u < 2; ++u)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t byte = vs[u] >> (8 * i) & 0xffu;
+      const bool nan = byte > kKvMaxExp + 127;
+      odd |= nan ? 1u << (4 * u + i) : 0u;
+      sc[u][i] = kv_scale(nan ? 127u : byte);
+    }
+  uint32_t nan = 0;  // bit 4 t + i: the row sees a NaN in the columns o[t][..][i]
+  if (__ballot(odd != 0)) {
+    // Token 16 u + 4 g' + i is NaN in the columns of lane (n', g').  The columns o[..][..][n] of a
+    // lane are those of n' = 4 g + n.
+    for (int u = 0; u < 2; ++u)
+      for (int gg = 0; gg < 4; ++gg)
+        for (int i = 0; i < 4; ++i) {
+          const int j = tok + 16 * u + 4 * gg + i;
+          for (int n = 0; n < 4; ++n) {
+            const uint32_t there = __shfl(odd, gg * 16 + 4 * g + n);
+            if (there >> (4 * u + i) & 1u) {
+#pragma unroll
+              for (int t = 0; t < QT; ++t)
+                if (sees(a, w.pos[t], j)) nan |= 1u << (4 * t + n);
+            }
+          }
+        }
+  }
+  bf16x8 part[QT][3];
+#pragma unroll
+  for (int t = 0; t < QT; ++t) {
+    const float e[8] = {p[t][0][0], p[t][0][1], p[t][0][2], p[t][0][3], p[t][1][0], p[t][1][1], p[t][1][2], p[t][1][3]};
+    split8(e, part[t]);
+  }
+  wide_products<D, 0, QT>(w, v, sc, part);
+#pragma unroll
+  for (int t = 0; t < QT; ++t)
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (nan >> (4 * t + i) & 1u) {
+#pragma unroll
+        for (int j = 0; j < D / 16; ++j) w.o[t][j][i] = __builtin_nanf("");
+      }
+}
+
+template <int D, int C, int QT, int NP>
+__device__ __forceinline__ void products(KvSums<D, QT>& w, const uint32_t (&v)[2][D / 32], const float (&sc)[2][4],
+                                         const f16x8 (&part)[QT][NP]) {
+  f16x8 f[2];
+  value_operands<D, C, true>(v, sc, f);
+#pragma unroll
+  for (int t = 0; t < QT; ++t)
+#pragma unroll
+    for (int n = NP - 1; n >= 0; --n)
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+        w.o[t][2 * C + j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f[j], part[t][n], w.o[t][2 * C + j], 0, 0, 0);
+  if constexpr (C + 1 < D / 32) products<D, C + 1, QT, NP>(w, v, sc, part);
+}
+
+// ---- kernels ----------------------------------------------------------------------------------
+
+// Waves of a SIMD of the rows' kernel, which is blocks of a compute unit: what the registers
+// of its loop allow.
+constexpr int kv_rows_waves(int d, int qt) { return d * qt == 64 ? 3 : 2; }
+// Tokens of a unit, and the units that a tile costs besides its own.
+constexpr int kKvRowsUnit = 128, kKvRowsLead = 3, kKvPromptLead = 3;
+constexpr int kv_prompt_unit(int d) { return d == 256 ? 32 : 64; }
+// Tiles of 16 rows of a wave of the prompt's kernel.
+constexpr int kv_prompt_qt(int d, bool bf16) { return d == 64 || (d == 128 && bf16) ? 2 : 1; }
+
+template <int D> hipError_t launch_kv_rows_attention(const KvAttentionArgs& a, int qt, bool bf16, hipStream_t s);
+template <int D> hipError_t launch_kv_prompt_attention(const KvAttentionArgs& a, bool bf16, hipStream_t s);
+
+}  // namespace cats

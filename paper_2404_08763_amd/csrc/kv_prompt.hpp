@@ -1,0 +1,245 @@
+// Attention over the cache in 4 bits for many rows of each sequence: a prompt.
+//
+// A block has a tile of 64 or 128 rows, each wave 16 QT of its own.  What a step of the keys
+// costs besides the products is the conversion of the cache, so it is done once for the
+// tile: each wave makes the operands of one record and puts them into LDS as its readers
+// take them, 16 bytes to a lane side by side, while the step before is multiplied (two
+// buffers, one barrier a step).  Of a wave's time per 32 tokens the products take 1/2 (32 of
+// 16 cycles for 32 rows), the softmax as much, the operands' reads from LDS a half of that.
+#pragma once
+
+#include "kv_attention.hpp"
+
+namespace cats {
+namespace {
+
+constexpr int kPromptLead = kKvPromptLead;
+
+template <int D, bool BF16> struct PromptSizes {
+  static constexpr int QT = kv_prompt_qt(D, BF16);
+  static constexpr int R = kKvWaves * 16 * QT;
+  static constexpr int RECS = D == 256 ? 2 : 4;  // records of a step
+  static constexpr int UNIT = RECS * kKvGroup;
+  static_assert(UNIT == kv_prompt_unit(D), "the host shares out the kernel's units");
+  static constexpr int NQ = BF16 ? 1 : 3, NP = BF16 ? 1 : 2;
+  static constexpr int KOPS = RECS * (D / 32), VOPS = RECS / 2 * (D / 16);  // operands of a step, 1 KB each
+  static constexpr int PART = R * (D + 2);
+};
+
+// One record's words, or (two records a step) the keys' or the values' of one.
+template <int D> struct Raw {
+  uint32_t k[D / 32], v[D / 32];
+  uint32_t ks, vs, bad;
+};
+
+// The values' operands of a record: the lower or upper half of each of a pair's.
+template <int D, int C> __device__ __forceinline__ void put_values(const uint32_t (&v)[D / 32], const float (&sc)[4], uint8_t* to) {
+  uint32_t e[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) e[i] = value_pair<D, C, true>(v, i, sc[i]);
+  *reinterpret_cast<u32x2*>(to + 2 * C * 1024) = u32x2{low_halves(e[0], e[1]), low_halves(e[2], e[3])};
+  *reinterpret_cast<u32x2*>(to + (2 * C + 1) * 1024) = u32x2{high_halves(e[0], e[1]), high_halves(e[2], e[3])};
+  if constexpr (C + 1 < D / 32) put_values<D, C + 1>(v, sc, to);
+}
+
+// A barrier that waits for LDS alone: the next records stay under way.
+__device__ __forceinline__ void lds_barrier() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
+template <int D, bool BF16> __global__ __launch_bounds__(kKvThreads, 2) void k_kv_prompt(KvAttentionArgs a) {
+  typedef PromptSizes<D, BF16> Z;
+  constexpr int QT = Z::QT, R = Z::R;
+  __shared__ __attribute__((aligned(16))) uint8_t lds[2][(Z::KOPS + Z::VOPS) * 1024];
+  __shared__ uint32_t wide[2][Z::RECS];
+  __shared__ int sh[8];
+  const int wave = uniform_u32(threadIdx.x / 64), lane = threadIdx.x % 64, g = lane / 16;
+  const int G = a.hq / a.hkv;
+  const KvLane<D> off;
+  const int rec = wave % Z::RECS;  // the wave's record of a step
+  const bool with_k = Z::RECS == 4 || wave < 2, with_v = Z::RECS == 4 || wave >= 2;
+  KvRun run;
+  if (!kv_run<true, Z::UNIT, kPromptLead, R>(a, run, sh)) return;
+
+  while (run.p < run.p1) {
+    const KvTile tile = kv_tile_of<true, Z::UNIT, R>(a, G, run);
+    const KvPart p = kv_part<kPromptLead>(run, tile);
+    if (p.u0 >= p.u1) {
+      kv_next<true, kPromptLead>(a, run, tile, p);
+      continue;
+    }
+    const int h = run.h;
+
+    // the wave's rows
+    KvSums<D, QT> w;
+    bf16x8 q[QT][Z::NQ][D / 32];
+    const int mine = wave * 16 * QT;
+#pragma unroll
+    for (int t = 0; t < QT; ++t) {
+      const int r = min(mine + t * 16 + lane % 16, tile.rows - 1);  // (rows behind the last repeat it and are not stored)
+      const int i = (tile.row0 + r) / G, head = h * G + (tile.row0 + r) % G;
+      w.pos[t] = tile.len - tile.nq + i;
+      w.m[t] = kLow;
+      w.l[t] = 0.f;
+      const size_t at = ((size_t)(tile.start + i) * a.hq + head) * D + g * (D / 4);
+#pragma unroll
+      for (int j = 0; j < D / 32; ++j) {
+        bf16x8 part[Z::NQ];
+        load_q8<Z::NQ>(a.q, at + 8 * j, part);
+#pragma unroll
+        for (int n = 0; n < Z::NQ; ++n) q[t][n][j] = part[n];
+      }
+#pragma unroll
+      for (int j = 0; j < D / 16; ++j) w.o[t][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    // positions of its first and last row; none: a last one that sees nothing
+    const int base = tile.len - tile.nq;
+    const int first = base + (tile.row0 + min(mine, tile.rows - 1)) / G;
+    const int last = mine < tile.rows ? base + (tile.row0 + min(mine + 16 * QT, tile.rows) - 1) / G : -1;
+
+    const KvRecords<D> records(a, tile.b, h, tile.hi);
+    const uint32_t rec0 = (uint32_t)tile.lo / kKvGroup + rec;
+    typename KvRecords<D>::Place place = records.find(rec0 + p.u0 * Z::RECS);
+    Raw<D> raw;
+    const auto load = [&](int u) {  // unit u, whose place is known; then the next one's place
+      const __amdgpu_buffer_rsrc_t r = records.at(place);
+      raw.bad = records.bad(place);
+      if (with_k) {
+        load_words<D / 32, false>(r, off.k, raw.k);
+        raw.ks = load_key_scales<D>(r, off.ks);
+      }
+      if (with_v) {
+        load_words<D / 32, false>(r, off.v, raw.v);
+        raw.vs = __builtin_amdgcn_raw_buffer_load_b32(r, (int)off.vs, 0, 0);
+      }
+      place = records.find(rec0 + (u + 1) * Z::RECS);
+    };
+    const auto put = [&](int u, int b) {
+      uint8_t* to = lds[b];
+      if (with_k) {
+        const uint32_t ks = raw.ks | raw.bad;
+#pragma unroll
+        for (int j = 0; j < D / 32; ++j)
+          reinterpret_cast<bf16x8*>(to)[(rec * (D / 32) + j) * 64 + lane] =
+              eight_of(raw.k[j], D == 256 && j >= 4 ? kv_scale(ks >> 8 & 0xffu) : kv_scale(ks & 0xffu));
+      }
+      if (with_v) {
+        const int tok = tile.lo + (u * Z::RECS + rec) * kKvGroup;
+        uint32_t vs = raw.vs;
+        if (tok + kKvGroup > tile.hi) vs = hidden_as_one(vs, tok + 4 * g, tile.hi);
+        const uint64_t odd = __ballot(not_narrow(vs) != 0);
+        if (lane == 0) wide[b][rec] = odd != 0 ? 1u : 0u;
+        if (__builtin_expect(odd != 0, 0)) no_values(raw.v, vs);
+        float sc[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sc[i] = kv_scale(vs >> (8 * i) & 0xffu);
+        put_values<D, 0>(raw.v, sc, to + Z::KOPS * 1024 + rec / 2 * (D / 16) * 1024 + lane * 16 + rec % 2 * 8);
+      }
+    };
+
+    load(p.u0);
+    put(p.u0, 0);
+    load(p.u0 + 1);
+    lds_barrier();
+    for (int u = p.u0; u < p.u1; ++u) {
+      const int b = (u - p.u0) & 1;
+      if (u + 1 < p.u1) {
+        put(u + 1, b ^ 1);
+        load(u + 2);
+      }
+#pragma unroll
+      for (int pair = 0; pair < Z::RECS / 2; ++pair) {
+        const int tok = tile.lo + u * Z::UNIT + pair * 32;
+        if (tok > last || (a.window > 0 && tok + 31 <= first - a.window)) continue;  // none of the wave's rows sees them
+        const bf16x8* ko = reinterpret_cast<const bf16x8*>(lds[b]) + pair * 2 * (D / 32) * 64 + lane;
+        const f16x8* vo = reinterpret_cast<const f16x8*>(lds[b] + Z::KOPS * 1024) + pair * (D / 16) * 64 + lane;
+        f32x4 z[QT][2];
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+#pragma unroll
+          for (int t = 0; t < QT; ++t) z[t][s] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int j = 0; j < D / 32; ++j) {
+            const bf16x8 k = ko[(s * (D / 32) + j) * 64];
+#pragma unroll
+            for (int n = Z::NQ - 1; n >= 0; --n)
+#pragma unroll
+              for (int t = 0; t < QT; ++t) z[t][s] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, q[t][n][j], z[t][s], 0, 0, 0);
+          }
+        }
+        const bool odd = uniform_u32(wide[b][2 * pair] | wide[b][2 * pair + 1]) != 0;
+        weights<D, QT>(w, a, z, tok, !(tok + 31 <= first && (a.window <= 0 || tok > last - a.window)));
+        if (__builtin_expect(odd, 0)) {
+          asm volatile("");
+          uint32_t v[2][D / 32], vs[2];
+#pragma unroll
+          for (int s = 0; s < 2; ++s) {
+            const __amdgpu_buffer_rsrc_t r = records.at(records.find((uint32_t)tok / kKvGroup + s));
+            load_words<D / 32, false>(r, off.v, v[s]);
+            vs[s] = hidden_as_one(__builtin_amdgcn_raw_buffer_load_b32(r, (int)off.vs, 0, 0), tok + 16 * s + 4 * g, tile.hi);
+            if (wide[b][2 * pair + s] == 0u) no_values(v[s], vs[s]);  // (its operands are in LDS)
+          }
+          wide_values<D, QT>(w, a, v, vs, z, tok);
+        }
+        f16x8 part[QT][Z::NP];
+        weight_operands<QT, Z::NP>(z, part);
+#pragma unroll
+        for (int j = 0; j < D / 16; ++j) {
+          const f16x8 v = vo[j * 64];
+#pragma unroll
+          for (int n = Z::NP - 1; n >= 0; --n)
+#pragma unroll
+            for (int t = 0; t < QT; ++t) w.o[t][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, part[t][n], w.o[t][j], 0, 0, 0);
+        }
+      }
+      lds_barrier();
+    }
+
+    float* part = a.part + ((size_t)run.lb * 2 + (p.head ? 1 : 0)) * Z::PART;
+#pragma unroll
+    for (int t = 0; t < QT; ++t) {
+      float l = w.l[t];
+      l += __shfl_xor(l, 16);
+      l += __shfl_xor(l, 32);
+      const int r = mine + t * 16 + lane % 16;
+      if (r >= tile.rows) continue;
+      const int i = (tile.row0 + r) / G;
+      const bool empty = w.pos[t] < 0;  // sees no key: zeros
+      const size_t at = ((size_t)(tile.start + i) * a.hq + h * G + (tile.row0 + r) % G) * D + g * (D / 4);
+      const float inv = p.whole ? 1.f / l : 1.f;
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+#pragma unroll
+        for (int j = 0; j < D / 16; j += 4) {
+          f32x4 o = f32x4{w.o[t][j][c], w.o[t][j + 1][c], w.o[t][j + 2][c], w.o[t][j + 3][c]} * inv;
+          if (p.whole) {
+            if (empty) o = f32x4{0.f, 0.f, 0.f, 0.f};
+            store_out<BF16>(a.out, at + c * (D / 16) + j, o);
+          } else {
+            *reinterpret_cast<f32x4*>(part + r * D + g * (D / 4) + c * (D / 16) + j) = o;
+          }
+        }
+      if (!p.whole && g == 0) {
+        part[R * D + r] = empty ? -__builtin_inff() : w.m[t];
+        part[R * D + R + r] = l;
+      }
+    }
+    kv_next<true, kPromptLead>(a, run, tile, p);
+  }
+}
+
+template <int D, bool BF16> hipError_t go_prompt(const KvAttentionArgs& a, hipStream_t s) {
+  KernelTimer tm("kv_attention", s);
+  hipExtLaunchKernelGGL((k_kv_prompt<D, BF16>), dim3(a.blocks), dim3(kKvThreads), 0, s, tm.start(), tm.stop(), 0, a);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+template <int D> hipError_t launch_kv_prompt_attention(const KvAttentionArgs& a, bool bf16, hipStream_t s) {
+  return bf16 ? go_prompt<D, true>(a, s) : go_prompt<D, false>(a, s);
+}
+
+}  // namespace cats

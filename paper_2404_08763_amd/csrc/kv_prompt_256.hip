@@ -1,0 +1,6 @@
+// Attention over the cache, many rows of each sequence, heads of 256 columns.
+#include "kv_prompt.hpp"
+
+namespace cats {
+template hipError_t launch_kv_prompt_attention<256>(const KvAttentionArgs& a, bool bf16, hipStream_t s);
+}  // namespace cats

@@ -107,12 +107,16 @@ def attention(q, ks, vs, lens, q_start, window, scale):
     bits -> (out, bound): bound is how far fp32 out may be off (rows of no sequence: NaN
     in both).  A weight p is off by the score's error (the fp32 sum of d products, its
     multiplication with the scale and the one with log2(e): |q| . |k| scale (d + 4) 2^-24 each way),
-    the exponential's (2^-21), the sums' (tokens 2^-24 at most) and its split's (2^-15 in
-    bf16, 2^-22 in fp32), all relative; out by that times sum p |v|, and its own rounding."""
+    the exponential's (2^-21), the sums' (tokens 2^-24 at most) and, as it enters the
+    second product, its rounding to f16, half a step: 2^-11 for bf16 rows; for fp32 rows
+    what that leaves is rounded again, 2^-22; all relative.  f16's steps are of one size
+    below 2^-14: half of one is 2^-25, with weights that are counted from 2^-7 of the
+    largest, so 2^-32 of that one's.  out is off by these times sum p |v|, the last by 2^-32
+    of the largest weight times sum |v|, and by its own rounding."""
     N, hq, d = q.shape
     out = torch.full((N, hq, d), math.nan, dtype=torch.float64)
     bound = torch.full_like(out, math.nan)
-    cut = 2.0 ** -15 if q.dtype is BF16 else 2.0 ** -22
+    cut = 2.0 ** -11 if q.dtype is BF16 else 2.0 ** -22
     for b, n in enumerate(lens):
         rows = range(b, b + 1) if q_start is None else range(q_start[b], q_start[b + 1])
         G = hq // ks[b].shape[1] if len(ks[b]) else 1
@@ -130,13 +134,14 @@ def attention(q, ks, vs, lens, q_start, window, scale):
             size = (k.abs() * q[r].double().abs()).sum(dim=-1).amax(dim=0) * scale
             rel = 2 * (d + 4) * 2.0 ** -24 * size + 2.0 ** -21 + 2 * (len(k) + 64) * 2.0 ** -24 + cut
             bound[r] = (p[..., None] * v.abs()).sum(dim=0) * rel[:, None] + out[r].abs() * HALF[q.dtype]
+            bound[r] += 2.0 ** -32 * p.amax(dim=0)[:, None] * v.abs().sum(dim=0)
     return out, bound
 
 
 class Batch:
     """Sequences in a cache: keys and values, pages in a shuffled order, queries."""
 
-    def __init__(self, lens, hq, hkv, d, page, dtype, counts=None, seed=1, spare=2, peak=1.0):
+    def __init__(self, lens, hq, hkv, d, page, dtype, counts=None, seed=1, spare=2, peak=1.0, far=None):
         g = gen(seed)
         self.lens, self.counts, self.hq, self.hkv, self.d, self.page = lens, counts, hq, hkv, d, page
         need = [(n + page - 1) // page for n in lens]
@@ -149,6 +154,8 @@ class Batch:
             mine, ids = ids[:need[b]], ids[need[b]:]
             self.table[b, :need[b]] = torch.tensor(mine, dtype=torch.int32)
             k, v = (torch.randn((n, hkv, d), generator=g) for _ in range(2))
+            if far is not None:  # values of very different sizes
+                v *= 2.0 ** torch.tensor(far)[torch.randint(0, len(far), (n, hkv, 1), generator=g)]
             t = torch.arange(n)
             slots = torch.tensor(mine + [0])[t // page] * page + t % page
             put(self.cache, slots, k, v)

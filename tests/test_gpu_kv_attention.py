@@ -89,6 +89,17 @@ def test_scale_and_peaks(dtype):
     _check(b)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=IDS.get)
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("far", [(-19.0, 0.0), (14.0, -60.0), (-100.0, -17.0, 13.0, 100.0), (-30.0,)])
+def test_values_of_any_size(far, d, dtype):
+    """Scales inside, at the ends of and beyond f16's range, tokens of both sorts side by side."""
+    say("kv far values", far, d, dtype)
+    _check(Batch([200, 31, 64], 4, 2, d, 16, dtype, seed=50, far=far))
+    _check(Batch([100, 31], 4, 2, d, 16, dtype, counts=[60, 31], seed=51, far=far))
+    _check(Batch([100, 31], 2, 2, d, 16, dtype, counts=[12, 3], seed=52, far=far), window=40)
+
+
 def _poison(b, seq, token, what):
     """Gives a token's keys or values the scale NaN (in cache and reference)."""
     d, page = b.d, b.page
