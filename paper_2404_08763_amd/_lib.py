@@ -742,11 +742,13 @@ def kv_cache(pages: int, heads: int, d: int, page: int = 64, device="cuda") -> t
 
 def _kv(cache: torch.Tensor, device: int):
     """A cache's C structure, its heads and its columns."""
-    if cache.dim() != 4 or cache.shape[3] % _KV_RECORD:
+    if cache.dim() != 4:
+        raise ValueError(f"cache must be [pages, heads, page / 16, 17 d], has shape {list(cache.shape)}")
+    pages, heads, groups, rec = cache.shape
+    if rec % _KV_RECORD:
         raise ValueError(f"cache must be [pages, heads, page / 16, 17 d], has shape {list(cache.shape)}")
     if cache.dtype is not torch.uint8 or cache.get_device() != device or not cache.is_contiguous():
         _refuse("cache", cache, torch.uint8, device)
-    pages, heads, groups, rec = cache.shape
     d = rec // _KV_RECORD
     return _KvCache(cache.data_ptr(), pages, 16 * groups, heads, d), heads, d
 
@@ -756,15 +758,26 @@ def _on(name: str, t: Optional[torch.Tensor], dtype: torch.dtype, device: int) -
         _refuse(name, t, dtype, device)
 
 
-def _pitched(name: str, t: torch.Tensor, cols: int, device: int) -> int:
-    """The pitch of rows [N, cols] or [N, heads, d] whose columns are dense."""
-    if t.dtype is not torch.float32 and t.dtype is not torch.bfloat16:
+_ROW_TYPES = {torch.float32: CATS_F32, torch.bfloat16: CATS_BF16}
+
+
+def _row_type(name: str, t: torch.Tensor) -> int:
+    dt = _ROW_TYPES.get(t.dtype)
+    if dt is None:
         raise ValueError(f"{name} must be torch.float32 or torch.bfloat16, got {t.dtype}")
+    return dt
+
+
+def _pitch(name: str, t: torch.Tensor, device: int) -> int:
+    """The pitch of rows [N, cols] or [N, heads, d] whose columns are dense."""
     if t.get_device() != device:
         _refuse(name, t, t.dtype, device)
-    if t.stride(-1) != 1 or (t.dim() == 3 and t.shape[1] > 1 and t.stride(1) != t.shape[2]):
+    strides, shape = t.stride(), t.shape
+    if strides[-1] != 1 or (len(shape) == 3 and shape[1] > 1 and strides[1] != shape[2]):
         raise ValueError(f"{name}'s rows must be dense")
-    return t.stride(0) if t.shape[0] > 1 else (cols + 7) // 8 * 8
+    if shape[0] == 1:  # (a single row's stride is no pitch)
+        return (shape[1] * (shape[2] if len(shape) == 3 else 1) + 7) // 8 * 8
+    return strides[0]
 
 
 def qk_norm_rope(qkv: torch.Tensor, heads: int, kv_heads: int, d: int, pos: Optional[torch.Tensor] = None,
@@ -780,44 +793,59 @@ def qk_norm_rope(qkv: torch.Tensor, heads: int, kv_heads: int, d: int, pos: Opti
     N, cols = _two_dims(qkv, "qkv")
     if cols < (heads + kv_heads) * d:
         raise ValueError(f"qkv must have {(heads + kv_heads) * d} columns or more, has {cols}")
-    if not qkv.is_cuda:
-        raise ValueError("qkv must be a device tensor")
+    xt = _row_type("qkv", qkv)
     if out is None:
+        if not qkv.is_cuda:
+            raise ValueError("qkv must be a device tensor")
         dtype = qkv.dtype if dtype is None else dtype
-        out = tuple(torch.empty((N, h, d), dtype=dtype, device=qkv.device) for h in (heads, kv_heads))
-    q, k = out
-    dtype = q.dtype
+        q, k = (torch.empty((N, h, d), dtype=dtype, device=qkv.device) for h in (heads, kv_heads))
+    else:
+        q, k = out
+        if q.shape != (N, heads, d):
+            _shape_is(q, (N, heads, d), "q")
+        if k.shape != (N, kv_heads, d):
+            _shape_is(k, (N, kv_heads, d), "k")
     device = _device()
-    ld = _pitched("qkv", qkv, cols, device)
-    _shape_is(q, (N, heads, d), "q")
-    _shape_is(k, (N, kv_heads, d), "k")
-    rot = 0
+    ld = _pitch("qkv", qkv, device)
+    yt, qt = _row_type("q", q), q.dtype
+    if q.get_device() != device or not q.is_contiguous():
+        _refuse("q", q, qt, device)
+    if k.dtype is not qt or k.get_device() != device or not k.is_contiguous():
+        _refuse("k", k, qt, device)
+    rot, fp, pp = 0, None, None
     if freq is not None:
-        rot = 2 * freq.shape[0]
         if pos is None:
             raise ValueError("freq needs pos")
-        _shape_is(freq, (rot // 2,), "freq")
-        _shape_is(pos, (N,), "pos")
-        _on("freq", freq, torch.float32, device)
-        _on("pos", pos, torch.int32, device)
-    for name, t in (("gain_q", gain_q), ("gain_k", gain_k)):
-        if t is not None:
-            if not norm:
-                raise ValueError(f"{name} needs norm=True")
-            _shape_is(t, (d,), name)
-            _on(name, t, torch.float32, device)
-    _on("q", q, dtype, device)
-    _on("k", k, dtype, device)
-    _check(raw().cats_qk_norm_rope(qkv.data_ptr(), _wdtype(qkv.dtype), ld, N, heads, kv_heads, d, 1 if norm else 0,
-                                   _ptr(gain_q), _ptr(gain_k), eps, _ptr(pos) if rot else None, _ptr(freq), rot,
-                                   1 if interleaved else 0, q.data_ptr(), k.data_ptr(), _wdtype(dtype), _stream()))
+        half = freq.shape[0]
+        if freq.dim() != 1:
+            raise ValueError(f"freq must have one dimension, got shape {list(freq.shape)}")
+        if pos.shape != (N,):
+            _shape_is(pos, (N,), "pos")
+        if freq.dtype is not torch.float32 or freq.get_device() != device or not freq.is_contiguous():
+            _refuse("freq", freq, torch.float32, device)
+        if pos.dtype is not torch.int32 or pos.get_device() != device or not pos.is_contiguous():
+            _refuse("pos", pos, torch.int32, device)
+        rot = 2 * half
+        if rot:
+            fp, pp = freq.data_ptr(), pos.data_ptr()
+    if gain_q is not None or gain_k is not None:
+        if not norm:
+            raise ValueError("gain_q and gain_k need norm=True")
+        for name, t in (("gain_q", gain_q), ("gain_k", gain_k)):
+            if t is not None:
+                _shape_is(t, (d,), name)
+                _on(name, t, torch.float32, device)
+    _check((_lib or raw()).cats_qk_norm_rope(
+        qkv.data_ptr(), xt, ld, N, heads, kv_heads, d, 1 if norm else 0, _ptr(gain_q), _ptr(gain_k), eps, pp, fp, rot,
+        1 if interleaved else 0, q.data_ptr(), k.data_ptr(), yt, _stream()))
     return q, k
 
 
 def _slots_of(slots: torch.Tensor, device: int) -> int:
     if slots.dim() != 1:
         raise ValueError(f"slots must have one dimension, got shape {list(slots.shape)}")
-    _on("slots", slots, torch.int32, device)
+    if slots.dtype is not torch.int32 or slots.get_device() != device or not slots.is_contiguous():
+        _refuse("slots", slots, torch.int32, device)
     return slots.shape[0]
 
 
@@ -829,14 +857,18 @@ def kv_write(cache: torch.Tensor, k: torch.Tensor, v: torch.Tensor, slots: torch
     device = _device()
     c, heads, d = _kv(cache, device)
     N = _slots_of(slots, device)
-    for name, t in (("k", k), ("v", v)):
-        if t.shape != (N, heads, d) and t.shape != (N, heads * d):
-            raise ValueError(f"{name} must be {[N, heads, d]} or {[N, heads * d]}, has shape {list(t.shape)}")
-    if k.dtype != v.dtype:
+    whole, flat = (N, heads, d), (N, heads * d)
+    ks, vs = k.shape, v.shape
+    if ks != whole and ks != flat:
+        raise ValueError(f"k must be {list(whole)} or {list(flat)}, has shape {list(ks)}")
+    if vs != whole and vs != flat:
+        raise ValueError(f"v must be {list(whole)} or {list(flat)}, has shape {list(vs)}")
+    if k.dtype is not v.dtype:
         raise ValueError(f"k and v must have one type, got {k.dtype} and {v.dtype}")
-    ldk, ldv = _pitched("k", k, heads * d, device), _pitched("v", v, heads * d, device)
-    _check(raw().cats_kv_write(ctypes.byref(c), k.data_ptr(), ldk, v.data_ptr(), ldv, _wdtype(k.dtype), slots.data_ptr(),
-                               N, _stream()))
+    dt = _row_type("k", k)
+    ldk, ldv = _pitch("k", k, device), _pitch("v", v, device)
+    _check((_lib or raw()).cats_kv_write(ctypes.byref(c), k.data_ptr(), ldk, v.data_ptr(), ldv, dt, slots.data_ptr(), N,
+                                         _stream()))
 
 
 def kv_read(cache: torch.Tensor, slots: torch.Tensor, dtype: torch.dtype = torch.bfloat16, out=None):
@@ -849,10 +881,17 @@ def kv_read(cache: torch.Tensor, slots: torch.Tensor, dtype: torch.dtype = torch
     if out is None:
         out = tuple(torch.empty((N, heads, d), dtype=dtype, device=cache.device) for _ in range(2))
     k, v = out
-    for name, t in (("k", k), ("v", v)):
-        _shape_is(t, (N, heads, d), name)
-        _on(name, t, k.dtype, device)
-    _check(raw().cats_kv_read(ctypes.byref(c), slots.data_ptr(), N, k.data_ptr(), v.data_ptr(), _wdtype(k.dtype), _stream()))
+    shape = (N, heads, d)
+    if k.shape != shape:
+        _shape_is(k, shape, "k")
+    if v.shape != shape:
+        _shape_is(v, shape, "v")
+    dt, kt = _row_type("k", k), k.dtype
+    if k.get_device() != device or not k.is_contiguous():
+        _refuse("k", k, kt, device)
+    if v.dtype is not kt or v.get_device() != device or not v.is_contiguous():
+        _refuse("v", v, kt, device)
+    _check((_lib or raw()).cats_kv_read(ctypes.byref(c), slots.data_ptr(), N, k.data_ptr(), v.data_ptr(), dt, _stream()))
     return k, v
 
 
@@ -882,30 +921,40 @@ def kv_attention(q: torch.Tensor, cache: torch.Tensor, table: torch.Tensor, lens
     if dq != d:
         raise ValueError(f"q's heads have {dq} columns, the cache's {d}")
     B, width = _two_dims(table, "table")
-    _shape_is(lens, (B,), "lens")
+    if lens.shape != (B,):
+        _shape_is(lens, (B,), "lens")
+    starts = None
     if q_start is not None:
-        _shape_is(q_start, (B + 1,), "q_start")
+        if q_start.shape != (B + 1,):
+            _shape_is(q_start, (B + 1,), "q_start")
+        if q_start.dtype is not torch.int32 or q_start.get_device() != device or not q_start.is_contiguous():
+            _refuse("q_start", q_start, torch.int32, device)
+        starts = q_start.data_ptr()
     elif N != B:
         raise ValueError(f"without q_start q must have a row for each of {B} sequences, has {N}")
-    dtype = q.dtype
-    dt = _wdtype(dtype)
+    dt, dtype = _row_type("q", q), q.dtype
     if out is None:
         if not q.is_cuda:
             raise ValueError("q must be a device tensor")
         out = torch.empty_like(q, memory_format=torch.contiguous_format)
     else:
-        _shape_is(out, (N, heads, d), "out")
-    _on("q", q, dtype, device)
-    _on("out", out, dtype, device)
-    _on("table", table, torch.int32, device)
-    _on("lens", lens, torch.int32, device)
-    _on("q_start", q_start, torch.int32, device)
-    _on("ws", ws, torch.uint8, device)
+        if out.shape != q.shape:
+            _shape_is(out, (N, heads, d), "out")
+        if out.dtype is not dtype or out.get_device() != device or not out.is_contiguous():
+            _refuse("out", out, dtype, device)
+    if q.get_device() != device or not q.is_contiguous():
+        _refuse("q", q, dtype, device)
+    if table.dtype is not torch.int32 or table.get_device() != device or not table.is_contiguous():
+        _refuse("table", table, torch.int32, device)
+    if lens.dtype is not torch.int32 or lens.get_device() != device or not lens.is_contiguous():
+        _refuse("lens", lens, torch.int32, device)
     if ws is None:
         ws = kv_attention_workspace(N, B, heads, kv_heads, d, device=q.device)
-    _check(raw().cats_kv_attention(q.data_ptr(), dt, N, heads, ctypes.byref(c), table.data_ptr(), width, lens.data_ptr(),
-                                   _ptr(q_start), B, d ** -0.5 if scale is None else scale, window, out.data_ptr(),
-                                   ws.data_ptr(), ws.numel(), _stream()))
+    elif ws.dtype is not torch.uint8 or ws.get_device() != device or not ws.is_contiguous():
+        _refuse("ws", ws, torch.uint8, device)
+    _check((_lib or raw()).cats_kv_attention(
+        q.data_ptr(), dt, N, heads, ctypes.byref(c), table.data_ptr(), width, lens.data_ptr(), starts, B,
+        d ** -0.5 if scale is None else scale, window, out.data_ptr(), ws.data_ptr(), ws.numel(), _stream()))
     return out
 
 

@@ -295,7 +295,8 @@ struct KvRowsArgs {
   uint8_t* cache;        // [pages x heads x page / 16] records (kv4.hpp)
   const int* slots;      // [rows]; a row whose slot is outside [0, tokens) is left out
   int tokens;            // pages * page
-  int page, heads, rows;
+  int groups, heads, rows;  // groups: records of a page
+  uint32_t magic;        // ceil(2^31 / groups)
   const void* k;         // write: [rows x ldk], [rows x ldv]
   const void* v;
   size_t ldk, ldv;

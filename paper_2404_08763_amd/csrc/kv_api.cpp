@@ -69,6 +69,12 @@ cats_status check_cache(const cats_kv_cache* c) {
   return CATS_OK;
 }
 
+// For the quotient of a record's number (below 2^26) by the records of a page (16 at most):
+// rec / groups is the upper half of 2 rec ceil(2^31 / groups).  The factor is less than 16 / groups
+// above 2^31 / groups, so the product is above the quotient by less than 2^26 * 16 / 2^31 of
+// 1 / groups, and has its whole part.
+uint32_t magic_of(int groups) { return (uint32_t)(((1ull << 31) + groups - 1) / groups); }
+
 constexpr size_t kWsAlign = 256;
 
 // Queries of a call: whether N rows for B sequences of hq heads on hkv are within the limits.
@@ -155,7 +161,8 @@ cats_status cats_kv_write(const cats_kv_cache* cache, const void* k, int64_t ldk
   a.cache = static_cast<uint8_t*>(cache->data);
   a.slots = slots;
   a.tokens = cache->pages * cache->page;
-  a.page = cache->page;
+  a.groups = cache->page / 16;
+  a.magic = magic_of(a.groups);
   a.heads = cache->heads;
   a.rows = N;
   a.k = k;
@@ -185,7 +192,8 @@ cats_status cats_kv_read(const cats_kv_cache* cache, const int32_t* slots, int32
   a.cache = static_cast<uint8_t*>(cache->data);
   a.slots = slots;
   a.tokens = cache->pages * cache->page;
-  a.page = cache->page;
+  a.groups = cache->page / 16;
+  a.magic = magic_of(a.groups);
   a.heads = cache->heads;
   a.rows = N;
   a.k_out = k;
@@ -243,7 +251,7 @@ cats_status cats_kv_attention(const void* q, int32_t dtype, int32_t N, int32_t h
   a.pages = cache->pages;
   a.width = width;
   a.groups = cache->page / 16;
-  a.magic = (uint32_t)(((1ull << 31) + a.groups - 1) / a.groups);
+  a.magic = magic_of(a.groups);
   a.limit = width * cache->page;
   a.c = scale * 1.44269504088896340736f;
   a.window = window;

@@ -22,9 +22,9 @@ struct Place {
 template <int D> __device__ __forceinline__ bool place(const KvRowsArgs& a, int row, int head, Place& p) {
   const int slot = a.slots[row];
   if (slot < 0 || slot >= a.tokens) return false;
-  const int page = slot / a.page, in = slot - page * a.page;
-  p.rec = (((size_t)page * a.heads + head) * (a.page / kKvGroup) + in / kKvGroup) * kv_record_bytes(D);
-  p.t = in % kKvGroup;
+  const uint32_t rec = (uint32_t)slot / kKvGroup, page = __umulhi(rec << 1, a.magic);
+  p.rec = (((size_t)page * a.heads + head) * a.groups + (rec - page * a.groups)) * kv_record_bytes(D);
+  p.t = slot % kKvGroup;
   return true;
 }
 
@@ -37,88 +37,101 @@ template <int D> __device__ __forceinline__ int scale_at(bool value, int t, int 
   return 16 * D + (value ? D / 2 + ((t >> 2) * (D / 32) + blk) * 4 + (t & 3) : t * (D / 32) + blk);
 }
 
-template <int D, bool BF16> __global__ __launch_bounds__(kThreads) void k_kv_write(KvRowsArgs a) {
-  constexpr int L = D / 8;  // lanes of a row
-  const int row = blockIdx.x * (kThreads / L) + threadIdx.x / L, head = blockIdx.y, c = threadIdx.x % L;
-  const bool value = blockIdx.z != 0;
-  Place p;
-  // (all four lanes of a scale have the same row)
-  if (row >= a.rows || !place<D>(a, row, head, p)) return;
-  float f[8];
-  const size_t at = (size_t)row * (value ? a.ldv : a.ldk) + head * D + 8 * c;
-  const void* src = value ? a.v : a.k;
+// (rows are read once: non-temporal, which leaves the L2 to the records that fill up there)
+template <bool BF16> __device__ __forceinline__ void load8(const void* src, size_t at, float* f) {
   if (BF16) {
-    widen<wbf16>(*reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(src) + at), f);
+    widen<wbf16>(__builtin_nontemporal_load(reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(src) + at)), f);
   } else {
     const u32x4* s = reinterpret_cast<const u32x4*>(static_cast<const float*>(src) + at);
-    widen<wf32>(s[0], f);
-    widen<wf32>(s[1], f + 4);
+    widen<wf32>(__builtin_nontemporal_load(s), f);
+    widen<wf32>(__builtin_nontemporal_load(s + 1), f + 4);
   }
+}
+
+// Codes of a lane's 8 columns, with the scale of its four lanes' 32.
+__device__ __forceinline__ uint32_t codes_of(const float* f, uint32_t& byte) {
   uint32_t top = 0;
 #pragma unroll
   for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(f[i]) & 0x7fffffffu);
   top = max(top, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top, 0xb1, 0xf, 0xf, false));
   top = max(top, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top, 0x4e, 0xf, 0xf, false));
-  const uint32_t byte = kv_scale_byte(top);
+  byte = kv_scale_byte(top);
   const float s = kv_scale(byte);
   uint32_t w = 0;
   w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, f[0], f[1], s, 0);
   w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, f[2], f[3], s, 1);
   w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, f[4], f[5], s, 2);
   w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, f[6], f[7], s, 3);
-  if (byte == 255u) w = 0;  // (NaN by its scale; the codes of such a block are 0)
-  uint8_t* rec = a.cache + p.rec;
-  if (!value) {
-    *reinterpret_cast<uint32_t*>(rec + p.t * (D / 2) + 4 * c) = w;
-  } else if (D == 64) {
-    uint8_t* to = rec + value_at<D>(p.t, c);
-    *reinterpret_cast<uint16_t*>(to) = (uint16_t)w;
-    *reinterpret_cast<uint16_t*>(to + 8) = (uint16_t)(w >> 16);
-  } else {
-    *reinterpret_cast<uint32_t*>(rec + value_at<D>(p.t, c)) = w;
-  }
-  if (c % 4 == 0) rec[scale_at<D>(value, p.t, c / 4)] = (uint8_t)byte;
+  return byte == 255u ? 0u : w;  // (NaN by its scale; the codes of such a block are 0)
 }
 
-template <int D, bool BF16> __global__ __launch_bounds__(kThreads) void k_kv_read(KvRowsArgs a) {
-  constexpr int L = D / 8;
-  const int row = blockIdx.x * (kThreads / L) + threadIdx.x / L, head = blockIdx.y, c = threadIdx.x % L;
-  const bool value = blockIdx.z != 0;
+template <int D, bool BF16> __global__ __launch_bounds__(kThreads) void k_kv_write(KvRowsArgs a) {
+  constexpr int L = D / 8;  // lanes of a row
+  const uint32_t part = blockIdx.x / (uint32_t)a.heads;
+  const int row = part * (kThreads / L) + threadIdx.x / L, head = blockIdx.x - part * a.heads, c = threadIdx.x % L;
+  // (all four lanes of a scale have the same row)
+  if (row >= a.rows) return;
+  float k[8], v[8];
+  load8<BF16>(a.k, (size_t)row * a.ldk + head * D + 8 * c, k);
+  load8<BF16>(a.v, (size_t)row * a.ldv + head * D + 8 * c, v);
   Place p;
-  if (row >= a.rows || !place<D>(a, row, head, p)) return;
-  const uint8_t* rec = a.cache + p.rec;
-  uint32_t w;
-  if (!value) {
-    w = *reinterpret_cast<const uint32_t*>(rec + p.t * (D / 2) + 4 * c);
-  } else if (D == 64) {
-    const uint8_t* from = rec + value_at<D>(p.t, c);
-    w = *reinterpret_cast<const uint16_t*>(from) | (uint32_t)*reinterpret_cast<const uint16_t*>(from + 8) << 16;
+  if (!place<D>(a, row, head, p)) return;
+  uint8_t* rec = a.cache + p.rec;
+  uint32_t kb, vb;
+  const uint32_t kw = codes_of(k, kb), vw = codes_of(v, vb);
+  *reinterpret_cast<uint32_t*>(rec + p.t * (D / 2) + 4 * c) = kw;
+  uint8_t* to = rec + value_at<D>(p.t, c);
+  if (D == 64) {
+    *reinterpret_cast<uint16_t*>(to) = (uint16_t)vw;
+    *reinterpret_cast<uint16_t*>(to + 8) = (uint16_t)(vw >> 16);
   } else {
-    w = *reinterpret_cast<const uint32_t*>(rec + value_at<D>(p.t, c));
+    *reinterpret_cast<uint32_t*>(to) = vw;
   }
-  const float s = kv_scale(rec[scale_at<D>(value, p.t, c / 4)]);
-  void* dst = value ? a.v_out : a.k_out;
-  const size_t at = ((size_t)row * a.heads + head) * D + 8 * c;
+  if (c % 4 == 0) {
+    rec[scale_at<D>(false, p.t, c / 4)] = (uint8_t)kb;
+    rec[scale_at<D>(true, p.t, c / 4)] = (uint8_t)vb;
+  }
+}
+
+template <bool BF16> __device__ __forceinline__ void store8(void* dst, size_t at, uint32_t w, float s) {
   if (BF16) {
     u32x4 o;
     o.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 0));
     o.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 1));
     o.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 2));
     o.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 3));
-    *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(dst) + at) = o;
+    __builtin_nontemporal_store(o, reinterpret_cast<u32x4*>(static_cast<uint16_t*>(dst) + at));
   } else {
     const f32x2 v0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, s, 0);
     const f32x2 v1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, s, 1);
     const f32x2 v2 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, s, 2);
     const f32x2 v3 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, s, 3);
     f32x4* o = reinterpret_cast<f32x4*>(static_cast<float*>(dst) + at);
-    o[0] = f32x4{v0[0], v0[1], v1[0], v1[1]};
-    o[1] = f32x4{v2[0], v2[1], v3[0], v3[1]};
+    __builtin_nontemporal_store(f32x4{v0[0], v0[1], v1[0], v1[1]}, o);
+    __builtin_nontemporal_store(f32x4{v2[0], v2[1], v3[0], v3[1]}, o + 1);
   }
 }
 
+template <int D, bool BF16> __global__ __launch_bounds__(kThreads) void k_kv_read(KvRowsArgs a) {
+  constexpr int L = D / 8;
+  const uint32_t part = blockIdx.x / (uint32_t)a.heads;
+  const int row = part * (kThreads / L) + threadIdx.x / L, head = blockIdx.x - part * a.heads, c = threadIdx.x % L;
+  Place p;
+  if (row >= a.rows || !place<D>(a, row, head, p)) return;
+  const uint8_t* rec = a.cache + p.rec;
+  const uint32_t kw = *reinterpret_cast<const uint32_t*>(rec + p.t * (D / 2) + 4 * c);
+  const uint8_t* from = rec + value_at<D>(p.t, c);
+  const uint32_t vw = D == 64 ? *reinterpret_cast<const uint16_t*>(from) |
+                                    (uint32_t)*reinterpret_cast<const uint16_t*>(from + 8) << 16
+                              : *reinterpret_cast<const uint32_t*>(from);
+  const float ks = kv_scale(rec[scale_at<D>(false, p.t, c / 4)]), vs = kv_scale(rec[scale_at<D>(true, p.t, c / 4)]);
+  const size_t at = ((size_t)row * a.heads + head) * D + 8 * c;
+  store8<BF16>(a.k_out, at, kw, ks);
+  store8<BF16>(a.v_out, at, vw, vs);
+}
+
 template <int D> hipError_t go(bool write, bool bf16, const KvRowsArgs& a, hipStream_t s) {
-  const dim3 grid((a.rows + kThreads / (D / 8) - 1) / (kThreads / (D / 8)), a.heads, 2);
+  const dim3 grid((uint32_t)((a.rows + kThreads / (D / 8) - 1) / (kThreads / (D / 8))) * a.heads);
   KernelTimer tm(write ? "kv_write" : "kv_read", s);
 #define CATS_GO(K) hipExtLaunchKernelGGL((K), grid, dim3(kThreads), 0, s, tm.start(), tm.stop(), 0, a)
   if (write) {

@@ -18,17 +18,28 @@ namespace {
 
 constexpr int kThreads = 256;
 
-template <bool BF16> __device__ __forceinline__ void load4(const void* p, size_t at, float* f) {
-  if (BF16) {
-    const uint2 w = *reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(p) + at);
-    f[0] = __uint_as_float(w.x << 16);
-    f[1] = __uint_as_float(w.x & 0xffff0000u);
-    f[2] = __uint_as_float(w.y << 16);
-    f[3] = __uint_as_float(w.y & 0xffff0000u);
-  } else {
-    widen<wf32>(*reinterpret_cast<const u32x4*>(static_cast<const float*>(p) + at), f);
+// Four elements as they are in memory.
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+template <bool BF16> struct Quad;
+template <> struct Quad<true> {
+  u32x2 v;
+  __device__ __forceinline__ void load(const void* p, size_t at) {
+    v = *reinterpret_cast<const u32x2*>(static_cast<const uint16_t*>(p) + at);
   }
-}
+  __device__ __forceinline__ void get(float* f) const {
+    f[0] = __uint_as_float(v.x << 16);
+    f[1] = __uint_as_float(v.x & 0xffff0000u);
+    f[2] = __uint_as_float(v.y << 16);
+    f[3] = __uint_as_float(v.y & 0xffff0000u);
+  }
+};
+template <> struct Quad<false> {
+  u32x4 v;
+  __device__ __forceinline__ void load(const void* p, size_t at) {
+    v = *reinterpret_cast<const u32x4*>(static_cast<const float*>(p) + at);
+  }
+  __device__ __forceinline__ void get(float* f) const { widen<wf32>(v, f); }
+};
 
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 template <bool BF16> __device__ __forceinline__ void store4(void* p, size_t at, const float* f) {
@@ -62,6 +73,13 @@ template <int L, bool XB, bool YB> __global__ __launch_bounds__(kThreads) void k
   const bool mine = 8 * s < a.d, turns = 8 * s < a.rot;
   // columns of the lane's two quads
   const int ca = turns && !a.interleaved ? 4 * s : 8 * s, cb = turns && !a.interleaved ? 4 * s + a.rot / 2 : 8 * s + 4;
+  const int h0 = chunk * a.passes * HW + lane / L, end = min(H, (chunk + 1) * a.passes * HW);
+  const size_t x0 = (size_t)row * a.ld;
+  Quad<XB> nu, nw;  // the next pass's, loaded before this one's are used
+  if (mine && h0 < end) {
+    nu.load(a.x, x0 + (size_t)h0 * a.d + ca);
+    nw.load(a.x, x0 + (size_t)h0 * a.d + cb);
+  }
   float co[4] = {1.f, 1.f, 1.f, 1.f}, si[4] = {0.f, 0.f, 0.f, 0.f};
   if (turns) {
     const double pos = (double)a.pos[row];
@@ -72,13 +90,16 @@ template <int L, bool XB, bool YB> __global__ __launch_bounds__(kThreads) void k
       sincospif((float)(half - 2.0 * rint(0.5 * half)), &si[i], &co[i]);
     }
   }
-  for (int k = 0; k < a.passes; ++k) {
-    const int h = (chunk * a.passes + k) * HW + lane / L;
-    const bool on = mine && h < H;
+  for (int h = h0; h - lane / L < end; h += HW) {
+    const bool on = mine && h < end;
     float u[4] = {0.f, 0.f, 0.f, 0.f}, w[4] = {0.f, 0.f, 0.f, 0.f};
     if (on) {
-      load4<XB>(a.x, (size_t)row * a.ld + (size_t)h * a.d + ca, u);
-      load4<XB>(a.x, (size_t)row * a.ld + (size_t)h * a.d + cb, w);
+      nu.get(u);
+      nw.get(w);
+    }
+    if (mine && h + HW < end) {
+      nu.load(a.x, x0 + (size_t)(h + HW) * a.d + ca);
+      nw.load(a.x, x0 + (size_t)(h + HW) * a.d + cb);
     }
     if (a.norm) {
       float q = 0.f;
