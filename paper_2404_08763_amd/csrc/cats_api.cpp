@@ -806,6 +806,12 @@ bool gemv_shape_ok(int d, int n) {
 }
 }  // namespace
 
+extern "C++" {
+namespace cats {
+uint32_t call_epoch() { return next_epoch(); }
+}  // namespace cats
+}
+
 size_t cats_sparse_input_workspace_bytes(int32_t d, int32_t n, int32_t max_batch) {
   if (!gemv_shape_ok(d, n) || max_batch < 1 || max_batch > CATS_MAX_BATCH) return 0;
   return gemv_layout(d, n, max_batch).end;

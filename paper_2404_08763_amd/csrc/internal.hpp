@@ -14,6 +14,8 @@ namespace cats {
 
 // Records the message of a failed call on this thread and returns its status.
 cats_status report_error(cats_status st, const char* msg);
+// A tag for a ticketed call (ticket.hpp), never 0.
+uint32_t call_epoch();
 // What an enqueue-only call returns once its launches are out: CATS_OK, or with
 // CATS_SYNC_CHECK set the status of the synchronised stream.
 cats_status enqueued(void* stream, const char* what);
@@ -328,7 +330,10 @@ struct KvAttentionArgs {
   KvPlanEntry* plan;
   int* prefix;           // what is in front of each tile (KvRun)
   int* first;            // [B + 1] first tile of each sequence
-  int4* desc;            // [blocks] the sum that begins in each block
+  int parts;             // without a plan: parts of a tile that tickets join (64 KB); 0: a last kernel does
+  uint32_t epoch;        // the tickets' tag
+  unsigned long long* tickets;  // [blocks] of the sum that begins in each block
+  int4* desc;            // [blocks] the same's place, for the last kernel
   float* part;           // [blocks x 2] partial sums
 };
 // Workspace of a call, and at most of any call of up to N rows and B sequences.

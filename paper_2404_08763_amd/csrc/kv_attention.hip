@@ -58,7 +58,7 @@ __global__ __launch_bounds__(kPlanThreads) void k_kv_plan(KvAttentionArgs a, int
       }
       b = lo;
       row0 = (e - a.first[b]) * R;
-      u = kv_tile<UNIT>(a, G, b, row0, R).units + LEAD;
+      u = kv_tile<UNIT>(a, G, b, row0, R, kv_length(a, b)).units + LEAD;
     }
     const int at = block_prefix<kPlanThreads>(u, total, sh) + units;
     if (e < tiles) {
@@ -228,6 +228,13 @@ hipError_t launch_kv_attention(KvAttentionArgs a, int d, bool bf16, hipStream_t 
   a.desc = reinterpret_cast<int4*>(ws + sh.off_desc);
   a.part = reinterpret_cast<float*>(ws + sh.off_part);
   a.tiles = (a.hq / a.hkv + sh.R - 1) / sh.R;
+  // The last block to arrive joins a tile's parts where they are 64 KB at most if all tiles are
+  // as long as the tables (tiles of very different lengths: KvRun); more of them a kernel of their own.
+  const int row_bytes = std::min(sh.R, a.hq / a.hkv) * d * 4;
+  const long long split_in = std::min<long long>(units_most(a, sh.unit), sh.blocks / ((long long)sh.tiles * a.hkv) + 2);
+  a.parts = !a.q_start && split_in * row_bytes <= (64 << 10) ? (64 << 10) / row_bytes : 0;
+  a.tickets = reinterpret_cast<unsigned long long*>(a.desc);
+  a.epoch = call_epoch();
   // no more blocks than units
   const double most = (double)sh.tiles * a.hkv * (double)(units_most(a, sh.unit) + sh.lead);
   a.blocks = most < sh.blocks ? ((int)most + 7) / 8 * 8 : sh.blocks;
@@ -243,7 +250,7 @@ hipError_t launch_kv_attention(KvAttentionArgs a, int d, bool bf16, hipStream_t 
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  const bool split = a.limit > sh.unit;  // (else every tile is one unit)
+  const bool split = a.parts == 0 && a.limit > sh.unit;  // (else every tile is one unit)
   return d == 64 ? go<64>(a, sh, bf16, split, s) : d == 128 ? go<128>(a, sh, bf16, split, s) : go<256>(a, sh, bf16, split, s);
 }
 

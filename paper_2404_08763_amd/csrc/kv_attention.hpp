@@ -44,13 +44,13 @@ template <int UNIT> __device__ __forceinline__ void kv_span(const KvAttentionArg
   t.lo &= ~(kKvGroup - 1);
   t.units = max(1, (t.hi - t.lo + UNIT - 1) / UNIT);
 }
-template <int UNIT> __device__ __forceinline__ KvTile kv_tile(const KvAttentionArgs& a, int G, int b, int row0, int R) {
+template <int UNIT> __device__ __forceinline__ KvTile kv_tile(const KvAttentionArgs& a, int G, int b, int row0, int R, int len) {
   KvTile t;
   t.b = b;
   t.row0 = row0;
   t.nq = kv_queries(a, b, t.start);
   t.rows = min(R, t.nq * G - row0);
-  t.len = kv_length(a, b);
+  t.len = len;
   kv_span<UNIT>(a, G, t);
   return t;
 }
@@ -66,20 +66,35 @@ __device__ __forceinline__ int wave_prefix(int x) {
   return x;
 }
 
-// Exclusive prefix of v over the block's threads and its total.
-template <int THREADS> __device__ __forceinline__ int block_prefix(int v, int& total, int* sh) {
-  const int w = threadIdx.x / 64, x = wave_prefix(v);
+__device__ __forceinline__ int wave_max(int x) {
+  x = max(x, __builtin_amdgcn_update_dpp(x, x, 0x111, 0xf, 0xf, false));
+  x = max(x, __builtin_amdgcn_update_dpp(x, x, 0x112, 0xf, 0xf, false));
+  x = max(x, __builtin_amdgcn_update_dpp(x, x, 0x114, 0xf, 0xf, false));
+  x = max(x, __builtin_amdgcn_update_dpp(x, x, 0x118, 0xf, 0xf, false));
+  x = max(x, __builtin_amdgcn_update_dpp(x, x, 0x142, 0xa, 0xf, false));
+  return max(x, __builtin_amdgcn_update_dpp(x, x, 0x143, 0xc, 0xf, false));  // lane 63 has it
+}
+
+// Exclusive prefix of v over the block's threads, its total and (sh for twice as many) the largest.
+template <int THREADS> __device__ __forceinline__ int block_prefix(int v, int& total, int* sh, int* top = nullptr) {
+  constexpr int W = THREADS / 64;
+  const int w = threadIdx.x / 64, x = wave_prefix(v), m = top ? wave_max(v) : 0;
   __syncthreads();
-  if (threadIdx.x % 64 == 63) sh[w] = x;
+  if (threadIdx.x % 64 == 63) {
+    sh[w] = x;
+    if (top) sh[W + w] = m;
+  }
   __syncthreads();
-  int before = 0;
+  int before = 0, most = 0;
   total = 0;
 #pragma unroll
-  for (int i = 0; i < THREADS / 64; ++i) {
+  for (int i = 0; i < W; ++i) {
     if (i < w) before += sh[i];
     total += sh[i];
+    if (top) most = max(most, sh[W + i]);
   }
   total = (int)uniform_u32(total);
+  if (top) *top = max(*top, (int)uniform_u32(most));
   return before + x - v;
 }
 
@@ -99,29 +114,44 @@ struct KvRun {
   uint64_t p, p1;      // the run
   int tiles;           // of a head, or (no plan) of a sequence
   int h, e, b, skip;   // head, tile (no plan: of sequence b), and where in the tile
+  int len;             // of the first tile's sequence, while it is known; -1
 };
 
 template <bool PLAN, int UNIT, int LEAD, int R>
 __device__ __forceinline__ bool kv_run(const KvAttentionArgs& a, KvRun& r, int* sh) {
   const int G = a.hq / a.hkv;
   r.tiles = PLAN ? a.head[0] : a.tiles;
-  const auto cost = [&](int b) { return b < a.B ? r.tiles * (kv_tile<UNIT>(a, G, b, 0, R).units + LEAD) : 0; };
+  int len = 0;
+  const auto cost = [&](int b) {
+    if (b >= a.B) return 0;
+    len = kv_length(a, b);
+    return r.tiles * (kv_tile<UNIT>(a, G, b, 0, R, len).units + LEAD);
+  };
+  r.len = -1;
   uint32_t W = 0;  // of a head
-  int mine = 0, before = 0;
+  int mine = 0, before = 0, top = 0;
   if constexpr (PLAN) {
     W = (uint32_t)a.head[1];
   } else {
     for (int base = 0; base < a.B; base += kKvThreads) {
       int total;
       mine = cost(base + threadIdx.x);
-      before = block_prefix<kKvThreads>(mine, total, sh);
+      before = block_prefix<kKvThreads>(mine, total, sh, &top);
       W += (uint32_t)total;
     }
   }
   const uint64_t T = (uint64_t)W * (uint32_t)a.hkv;
-  const uint32_t nb = T < (uint32_t)a.blocks ? (uint32_t)T : (uint32_t)a.blocks;
+  uint32_t nb = T < (uint32_t)a.blocks ? (uint32_t)T : (uint32_t)a.blocks;
+  if (!PLAN && a.parts > 0) {
+    // A tile in a.parts parts at most, or, where it is long, in as many as it takes about as long
+    // to join (0.04 us a KB) as to read the keys of one of them (0.5 us a unit).
+    const uint32_t one = (uint32_t)(top / r.tiles);
+    const float longest = __builtin_sqrtf((float)one * (float)a.parts * (1.f / 5.f));
+    const uint64_t most = T * (uint32_t)(max(a.parts, (int)longest) - 1);
+    if ((uint64_t)nb * one > most) nb = quotient(most, one);
+  }
   r.lb = nb < (uint32_t)a.blocks ? (int)blockIdx.x : (int)((blockIdx.x % 8) * (nb / 8) + blockIdx.x / 8);
-  if (threadIdx.x == 0) a.desc[r.lb] = int4{0, 0, 0, 0};
+  if (a.parts == 0 && threadIdx.x == 0) a.desc[r.lb] = int4{0, 0, 0, 0};
   if ((uint32_t)r.lb >= nb) return false;
   r.base = quotient(T, nb);
   r.rem = (uint32_t)(T - (uint64_t)r.base * nb);
@@ -150,17 +180,19 @@ __device__ __forceinline__ bool kv_run(const KvAttentionArgs& a, KvRun& r, int* 
       }
       const uint32_t at = sum + (uint32_t)before;
       if (at <= x && x < at + (uint32_t)mine) {
-        sh[4] = base + threadIdx.x;
-        sh[5] = (int)(x - at);
-        sh[6] = mine;
+        sh[8] = base + threadIdx.x;
+        sh[9] = (int)(x - at);
+        sh[10] = mine;
+        sh[11] = len;
       }
       sum += (uint32_t)total;
       if (a.B <= kKvThreads || x < sum) break;
     }
     __syncthreads();
-    r.b = (int)uniform_u32(sh[4]);
-    const uint32_t in = uniform_u32(sh[5]), one = uniform_u32(sh[6]) / r.tiles;
+    r.b = (int)uniform_u32(sh[8]);
+    const uint32_t in = uniform_u32(sh[9]), one = uniform_u32(sh[10]) / r.tiles;
     r.e = (int)(in / one);
+    r.len = (int)uniform_u32(sh[11]);
     r.skip = (int)(in - r.e * one);
   }
   r.h = (int)uniform_u32(r.h);
@@ -172,9 +204,10 @@ __device__ __forceinline__ bool kv_run(const KvAttentionArgs& a, KvRun& r, int* 
 template <bool PLAN, int UNIT, int R> __device__ __forceinline__ KvTile kv_tile_of(const KvAttentionArgs& a, int G, const KvRun& r) {
   if constexpr (PLAN) {
     const KvPlanEntry t = a.plan[r.e];
-    return kv_tile<UNIT>(a, G, (int)uniform_u32(t.b), (int)uniform_u32(t.row0), R);
+    const int b = (int)uniform_u32(t.b);
+    return kv_tile<UNIT>(a, G, b, (int)uniform_u32(t.row0), R, kv_length(a, b));
   } else {
-    return kv_tile<UNIT>(a, G, r.b, r.e * R, R);
+    return kv_tile<UNIT>(a, G, r.b, r.e * R, R, r.len >= 0 ? r.len : kv_length(a, r.b));
   }
 }
 
@@ -194,17 +227,33 @@ template <int LEAD> __device__ __forceinline__ KvPart kv_part(const KvRun& r, co
   return p;
 }
 
-// Notes a sum that begins in this block and ends in a later one, and goes on to the next tile.
+// The block that has a place on the line.
+__device__ __forceinline__ int block_at(const KvRun& r, uint64_t x) {
+  const uint64_t big = (uint64_t)r.rem * (r.base + 1);
+  return (int)(x < big ? quotient(x, r.base + 1) : r.rem + quotient(x - big, r.base));
+}
+
+// The first of the blocks that have parts of the tile, and how many.
+template <int LEAD> __device__ __forceinline__ int kv_parts_of(const KvRun& r, const KvTile& t, const KvPart& p, int& n) {
+  const uint64_t from = r.p - (uint32_t)r.skip;
+  const int head = p.head ? r.lb : block_at(r, from + LEAD);
+  n = block_at(r, from + (uint32_t)(t.units + LEAD) - 1) - head + 1;
+  return head;
+}
+
+// Goes on to the next tile; before, notes for the last kernel (without tickets) a sum that
+// begins in this block and ends in a later one.
 template <bool PLAN, int LEAD>
 __device__ __forceinline__ void kv_next(const KvAttentionArgs& a, KvRun& r, const KvTile& t, const KvPart& p) {
   const uint64_t end = r.p - (uint32_t)r.skip + (uint32_t)(t.units + LEAD);  // of the tile, on the line
-  if (p.head && !p.whole && threadIdx.x == 0) {
-    const uint64_t x = end - 1, big = (uint64_t)r.rem * (r.base + 1);
-    const uint32_t until = x < big ? quotient(x, r.base + 1) : r.rem + quotient(x - big, r.base);
-    a.desc[r.lb] = int4{(int)until - r.lb + 1, r.h, t.b, t.row0};
+  if (a.parts == 0 && p.head && !p.whole && threadIdx.x == 0) {
+    int n;
+    kv_parts_of<LEAD>(r, t, p, n);
+    a.desc[r.lb] = int4{n, r.h, t.b, t.row0};
   }
   r.p = end < r.p1 ? end : r.p1;
   r.skip = 0;
+  r.len = -1;
   ++r.e;
   if constexpr (PLAN) {
     if (r.e == r.tiles) r.e = 0, ++r.h;

@@ -54,7 +54,7 @@ template <int D, bool BF16> __global__ __launch_bounds__(kKvThreads, 2) void k_k
   constexpr int QT = Z::QT, R = Z::R;
   __shared__ __attribute__((aligned(16))) uint8_t lds[2][(Z::KOPS + Z::VOPS) * 1024];
   __shared__ uint32_t wide[2][Z::RECS];
-  __shared__ int sh[8];
+  __shared__ int sh[12];
   const int wave = uniform_u32(threadIdx.x / 64), lane = threadIdx.x % 64, g = lane / 16;
   const int G = a.hq / a.hkv;
   const KvLane<D> off;

@@ -7,6 +7,7 @@
 #pragma once
 
 #include "kv_attention.hpp"
+#include "ticket.hpp"
 
 namespace cats {
 namespace {
@@ -139,6 +140,76 @@ __device__ __forceinline__ void step(Wave<D, QT, BF16>& w, const KvAttentionArgs
   values(s);
 }
 
+// The block that arrives last joins a tile's n parts: the first in block `first`, the others in
+// those behind it.  D / 4 threads have a row of a part; rows are side by side, and where there
+// are few of them, parts.
+template <int D, bool BF16>
+__device__ __forceinline__ void join_parts(const KvAttentionArgs& a, __amdgpu_buffer_rsrc_t parts, int first, int n, int size, int R,
+                                           const KvTile& tile, int h, uint8_t* lds) {
+  constexpr int L = D / 4, S = kThreads / L;
+  float (*so)[D] = reinterpret_cast<float (*)[D]>(lds);
+  float* sm = reinterpret_cast<float*>(lds) + S * D;
+  float* sl = sm + S;
+  const int s = threadIdx.x / L, c = threadIdx.x % L * 4, G = a.hq / a.hkv;
+  int side = 1;  // rows side by side
+  while (side < S && side < tile.rows) side *= 2;
+  const int sub = s / side, subs = S / side;
+  for (int r0 = 0; r0 < tile.rows; r0 += side) {
+    const int row = r0 + s % side;
+    float m = -__builtin_inff(), l = 0.f;
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+    if (row < tile.rows) {
+      // four parts' loads under way; one behind the last reads as zeros, and counts for none
+      for (int i0 = sub; i0 < n; i0 += 4 * subs) {
+        f32x4 po[4];
+        float pm[4], pl[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const int i = i0 + k * subs;
+          const uint32_t p = i < n ? (uint32_t)(2 * (first + i) + (i == 0 ? 1 : 0)) * (uint32_t)(size * 4) : kOOB;
+          po[k] = __builtin_bit_cast(f32x4, ld_buf16_coherent(parts, p + (row * D + c) * 4));
+          pm[k] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(parts, (int)(p + (R * D + row) * 4), 0, kCachePolicySc1));
+          pl[k] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(parts, (int)(p + (R * D + R + row) * 4), 0, kCachePolicySc1));
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const float is_m = i0 + k * subs < n ? pm[k] : -__builtin_inff();
+          const float top = fmaxf(m, is_m);
+          const float was = m == top ? 1.f : __builtin_amdgcn_exp2f(m - top);
+          const float is = is_m == top ? 1.f : __builtin_amdgcn_exp2f(is_m - top);
+          m = top;
+          l = l * was + pl[k] * is;
+          o = o * was + po[k] * is;
+        }
+      }
+    }
+    __syncthreads();
+    *reinterpret_cast<f32x4*>(&so[s][c]) = o;
+    if (c == 0) {
+      sm[s] = m;
+      sl[s] = l;
+    }
+    __syncthreads();
+    if (sub == 0 && row < tile.rows) {
+      float top = m;
+      for (int i = 1; i < subs; ++i) top = fmaxf(top, sm[s + i * side]);
+      l = 0.f;
+      o = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int i = 0; i < subs; ++i) {
+        const int from = s + i * side;
+        if (sm[from] == -__builtin_inff()) continue;  // (fewer parts than that, or a row that sees no key)
+        const float f = __builtin_amdgcn_exp2f(sm[from] - top);
+        l += sl[from] * f;
+        o += *reinterpret_cast<const f32x4*>(&so[from][c]) * f;
+      }
+      o *= 1.f / l;
+      if (top == -__builtin_inff()) o = f32x4{0.f, 0.f, 0.f, 0.f};
+      const int i = (tile.row0 + row) / G;
+      store_out<BF16>(a.out, ((size_t)(tile.start + i) * a.hq + h * G + (tile.row0 + row) % G) * D + c, o);
+    }
+  }
+}
+
 template <int D, int QT, bool BF16, bool PLAN>
 __global__ __launch_bounds__(kThreads, (Sizes<D, QT, BF16>::WAVES)) void k_kv_rows(KvAttentionArgs a) {
   typedef Sizes<D, QT, BF16> Z;
@@ -147,7 +218,7 @@ __global__ __launch_bounds__(kThreads, (Sizes<D, QT, BF16>::WAVES)) void k_kv_ro
   bf16x8* sq = reinterpret_cast<bf16x8*>(pool);
   float (*so)[16][Z::PITCH] = reinterpret_cast<float (*)[16][Z::PITCH]>(pool);
   __shared__ float sm[kWaves][R], sl[kWaves][R];
-  __shared__ int sh[8];
+  __shared__ int sh[13];
   const int wave = uniform_u32(threadIdx.x / 64), lane = threadIdx.x % 64, g = lane / 16;
   const int G = a.hq / a.hkv;
   const KvLane<D> off;
@@ -162,6 +233,13 @@ __global__ __launch_bounds__(kThreads, (Sizes<D, QT, BF16>::WAVES)) void k_kv_ro
       continue;
     }
     const int h = run.h, row0 = tile.row0, rows = tile.rows, start = tile.start;
+    // (the ticket's word is read now, so that arriving costs one atomic)
+    int n = 1, first_block = run.lb;
+    unsigned long long peek = 0;
+    if (!PLAN && a.parts > 0 && !p.whole) {
+      first_block = kv_parts_of<kLeadUnits>(run, tile, p, n);
+      if (threadIdx.x == 0) peek = ticket_peek(a.tickets + first_block);
+    }
     Wave<D, QT, BF16> w;
     load_q<D, QT, BF16>(w, a, h, tile, sq);
     const KvRecords<D> records(a, tile.b, h, tile.hi);
@@ -224,7 +302,9 @@ __global__ __launch_bounds__(kThreads, (Sizes<D, QT, BF16>::WAVES)) void k_kv_ro
         sl[wave][t * 16 + lane] = l;
       }
     }
-    float* part = a.part + ((size_t)run.lb * 2 + (p.head ? 1 : 0)) * Z::PART;
+    // where the part goes, in bytes from the first block's
+    const uint32_t part = (uint32_t)(run.lb * 2 + (p.head ? 1 : 0)) * (Z::PART * 4);
+    const __amdgpu_buffer_rsrc_t parts = make_rsrc(a.part, (uint32_t)a.blocks * 2 * (Z::PART * 4));
 #pragma unroll
     for (int t = 0; t < QT; ++t) {
       __syncthreads();
@@ -253,18 +333,35 @@ __global__ __launch_bounds__(kThreads, (Sizes<D, QT, BF16>::WAVES)) void k_kv_ro
         const int qi = (row0 + row) / G;
         const bool empty = tile.len - tile.nq + qi < 0;  // sees no key: zeros
         if (p.whole) {
-          const float inv = 1.f / l;
-          o *= inv;
+          o *= 1.f / l;
           if (empty) o = f32x4{0.f, 0.f, 0.f, 0.f};
           store_out<BF16>(a.out, ((size_t)(start + qi) * a.hq + h * G + (row0 + row) % G) * D + c, o);
         } else {
-          *reinterpret_cast<f32x4*>(part + row * D + c) = o;
-          if (c == 0) {
-            part[R * D + row] = empty ? -__builtin_inff() : m;
-            part[R * D + R + row] = l;
+          const uint32_t at = part + (row * D + c) * 4;
+          if (empty) m = -__builtin_inff();
+          if (PLAN || a.parts == 0) {
+            float* to = a.part + part / 4;
+            *reinterpret_cast<f32x4*>(to + row * D + c) = o;
+            if (c == 0) {
+              to[R * D + row] = m;
+              to[R * D + R + row] = l;
+            }
+          } else {
+            st_buf16_coherent(parts, at, __builtin_bit_cast(u32x4, o));
+            if (c == 0) {
+              __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(m), parts, (int)(part + (R * D + row) * 4), 0, kCachePolicySc1);
+              __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(l), parts, (int)(part + (R * D + R + row) * 4), 0, kCachePolicySc1);
+            }
           }
         }
       }
+    }
+    if (!PLAN && a.parts > 0 && !p.whole) {
+      __builtin_amdgcn_s_waitcnt(0);  // this thread's stores have completed
+      __syncthreads();
+      if (threadIdx.x == 0) sh[12] = take_ticket(a.tickets + first_block, a.epoch, (uint32_t)n, peek) ? 1 : 0;
+      __syncthreads();
+      if (sh[12]) join_parts<D, BF16>(a, parts, first_block, n, Z::PART, R, tile, h, pool);
     }
     __syncthreads();
     kv_next<PLAN, kLeadUnits>(a, run, tile, p);
