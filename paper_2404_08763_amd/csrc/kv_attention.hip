@@ -148,18 +148,18 @@ constexpr size_t up256(size_t v) { return (v + 255) / 256 * 256; }
 constexpr int kMostBlocks = 768;
 size_t part_bytes(int d, int R, int blocks) { return (size_t)blocks * 2 * R * (d + 2) * 4; }
 
-// Two to a compute unit; fewer where their partial sums would take more than 60 MiB.
+// Two to a compute unit; fewer where their partial sums would take more than 61 MiB.
 int prompt_blocks(int d) { return d == 64 ? 512 : 480; }
 
 Shape shape_of(int N, int B, int hq, int hkv, int d, bool bf16, bool planned) {
   Shape s{};
   const int G = hq / hkv;
   // A tile of 16 rows while it holds all of a sequence's rows, then 32; the prompt's kernel
-  // where its tiles of 64 or 128 are filled better than by half.
+  // for more.
   const long long per = planned ? ((long long)N * G + B - 1) / B : G;
   s.prompt = planned && per > 32;
   s.qt = per <= 16 || d == 256 ? 1 : 2;
-  s.R = s.prompt ? kKvWaves * 16 * kv_prompt_qt(d, bf16) : 16 * s.qt;
+  s.R = s.prompt ? kv_prompt_rows(d, bf16) : 16 * s.qt;
   s.unit = s.prompt ? kv_prompt_unit(d) : kKvRowsUnit;
   s.lead = s.prompt ? kKvPromptLead : kKvRowsLead;
   s.blocks = s.prompt ? prompt_blocks(d) : 256 * kv_rows_waves(d, s.qt);
@@ -209,7 +209,7 @@ size_t kv_attention_most(int N, int B, int hq, int hkv, int d) {
   const size_t tiles = ((size_t)N * (hq / hkv) + 15) / 16 + B;
   size_t part = 0;
   for (int qt = 1; qt <= 2; ++qt) part = std::max(part, part_bytes(d, 16 * qt, 256 * kv_rows_waves(d, qt)));
-  part = std::max(part, part_bytes(d, kKvWaves * 16 * kv_prompt_qt(d, true), prompt_blocks(d)));
+  part = std::max(part, part_bytes(d, kv_prompt_rows(d, true), prompt_blocks(d)));
   return 256 + up256(tiles * sizeof(KvPlanEntry)) + up256(tiles * 4) + up256((size_t)(B + 1) * 4) + up256(kMostBlocks * 16) + part;
 }
 

@@ -310,6 +310,15 @@ template <int D> struct KvRecords {
     const uint32_t at = __umulhi(rec << 1, magic);
     return Place{(uint32_t)scalar_load(table, at), (rec - at * groups) * kv_record_bytes(D)};
   }
+  // The same by a vector load, for a kernel whose waits for LDS would wait for scalar loads too;
+  // page is to be made uniform where it is used.
+  __device__ __forceinline__ Place find_later(uint32_t rec) const {
+    rec = min(rec, most);
+    const uint32_t at = __umulhi(rec << 1, magic);
+    const __amdgpu_buffer_rsrc_t t = make_rsrc(table, (at + 1) * 4);
+    return Place{(uint32_t)__builtin_amdgcn_raw_buffer_load_b32(t, (int)(at * 4), 0, 0),
+                 (rec - at * groups) * kv_record_bytes(D)};
+  }
   // All ones where the page is none of the cache's (whose first page is read for it).
   __device__ __forceinline__ uint32_t bad(const Place& p) const { return p.page < pages ? 0u : 0xffffu; }
   __device__ __forceinline__ __amdgpu_buffer_rsrc_t at(const Place& p) const {
@@ -457,15 +466,15 @@ template <int D, int QT> struct KvSums {
   int pos[QT];          // the row's position, -1 and less: sees nothing
 };
 
-// The softmax of a step: scores z of the tokens [tok, tok + 32) become weights, the sums
-// what they are counted from.  `masked`: not every row sees all of the tokens.
-template <int D, int QT>
-__device__ __forceinline__ void weights(KvSums<D, QT>& w, const KvAttentionArgs& a, f32x4 (&z)[QT][2], int tok, bool masked) {
+// The softmax of a step: scores z of the tokens of U records from tok on become weights, the
+// sums what they are counted from.  `masked`: not every row sees all of the tokens.
+template <int D, int QT, int U>
+__device__ __forceinline__ void weights(KvSums<D, QT>& w, const KvAttentionArgs& a, f32x4 (&z)[QT][U], int tok, bool masked) {
   const int g = threadIdx.x % 64 / 16;
   if (__builtin_expect(masked, 0)) {
     asm volatile("");  // (a branch: these cost a step a third more where no row needs them)
 #pragma unroll
-    for (int u = 0; u < 2; ++u)
+    for (int u = 0; u < U; ++u)
 #pragma unroll
       for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -478,7 +487,7 @@ __device__ __forceinline__ void weights(KvSums<D, QT>& w, const KvAttentionArgs&
   for (int t = 0; t < QT; ++t) {
     top[t] = z[t][0][0];
 #pragma unroll
-    for (int i = 1; i < 8; ++i) top[t] = fmaxf(top[t], z[t][i / 4][i % 4]);
+    for (int i = 1; i < 4 * U; ++i) top[t] = fmaxf(top[t], z[t][i / 4][i % 4]);
     top[t] *= a.c;
     rise |= top[t] > w.m[t] + (kLead + kLazy);  // (kLow plus that is kLow)
   }
@@ -499,7 +508,7 @@ __device__ __forceinline__ void weights(KvSums<D, QT>& w, const KvAttentionArgs&
   for (int t = 0; t < QT; ++t) {
     float l = 0.f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < 4 * U; ++i) {
       z[t][i / 4][i % 4] = __builtin_amdgcn_exp2f(fmaf(z[t][i / 4][i % 4], a.c, -w.m[t]));
       l += z[t][i / 4][i % 4];
     }
@@ -507,13 +516,14 @@ __device__ __forceinline__ void weights(KvSums<D, QT>& w, const KvAttentionArgs&
   }
 }
 
-// The weights as NP f16 parts, the second product's operands.
-template <int QT, int NP> __device__ __forceinline__ void weight_operands(const f32x4 (&z)[QT][2], f16x8 (&part)[QT][NP]) {
+// The weights of records `first` and the next as NP f16 parts, the second product's operands.
+template <int QT, int NP, int U>
+__device__ __forceinline__ void weight_operands(const f32x4 (&z)[QT][U], int first, f16x8 (&part)[QT][NP]) {
 #pragma unroll
   for (int t = 0; t < QT; ++t)
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      float r = z[t][i / 4][i % 4];
+      float r = z[t][first + i / 4][i % 4];
 #pragma unroll
       for (int n = 0; n < NP; ++n) {
         part[t][n][i] = (_Float16)r;
@@ -552,9 +562,9 @@ __device__ __forceinline__ void wide_products(KvSums<D, QT>& w, const uint32_t (
 // where nothing was written) become 1, and the rows that see such a token NaN in its columns.
 // The product of f16 operands follows in every step, here with values of 0 (no_values): where
 // it followed in other steps alone, every step copied the sums.
-template <int D, int QT>
+template <int D, int QT, int U>
 __device__ __forceinline__ void wide_values(KvSums<D, QT>& w, const KvAttentionArgs& a, const uint32_t (&v)[2][D / 32],
-                                         const uint32_t (&scales)[2], const f32x4 (&p)[QT][2], int tok) {
+                                            const uint32_t (&scales)[2], const f32x4 (&p)[QT][U], int first, int tok) {
   const int lane = threadIdx.x % 64, g = lane / 16;
   uint32_t odd = 0, vs[2] = {scales[0], scales[1]};
   float sc[2][4];
@@ -588,7 +598,8 @@ __device__ __forceinline__ void wide_values(KvSums<D, QT>& w, const KvAttentionA
   bf16x8 part[QT][3];
 #pragma unroll
   for (int t = 0; t < QT; ++t) {
-    const float e[8] = {p[t][0][0], p[t][0][1], p[t][0][2], p[t][0][3], p[t][1][0], p[t][1][1], p[t][1][2], p[t][1][3]};
+    const f32x4 x = p[t][first], y = p[t][first + 1];
+    const float e[8] = {x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
     split8(e, part[t]);
   }
   wide_products<D, 0, QT>(w, v, sc, part);
@@ -627,6 +638,7 @@ constexpr int kKvRowsUnit = 128, kKvRowsLead = 3, kKvPromptLead = 3;
 constexpr int kv_prompt_unit(int d) { return d == 256 ? 32 : 64; }
 // Tiles of 16 rows of a wave of the prompt's kernel.
 constexpr int kv_prompt_qt(int d, bool bf16) { return d == 64 || (d == 128 && bf16) ? 2 : 1; }
+constexpr int kv_prompt_rows(int d, bool bf16) { return kKvWaves * 16 * kv_prompt_qt(d, bf16); }
 
 template <int D> hipError_t launch_kv_rows_attention(const KvAttentionArgs& a, int qt, bool bf16, hipStream_t s);
 template <int D> hipError_t launch_kv_prompt_attention(const KvAttentionArgs& a, bool bf16, hipStream_t s);

@@ -17,7 +17,7 @@ constexpr int kPromptLead = kKvPromptLead;
 
 template <int D, bool BF16> struct PromptSizes {
   static constexpr int QT = kv_prompt_qt(D, BF16);
-  static constexpr int R = kKvWaves * 16 * QT;
+  static constexpr int R = kv_prompt_rows(D, BF16);
   static constexpr int RECS = D == 256 ? 2 : 4;  // records of a step
   static constexpr int UNIT = RECS * kKvGroup;
   static_assert(UNIT == kv_prompt_unit(D), "the host shares out the kernel's units");
@@ -101,9 +101,10 @@ template <int D, bool BF16> __global__ __launch_bounds__(kKvThreads, 2) void k_k
 
     const KvRecords<D> records(a, tile.b, h, tile.hi);
     const uint32_t rec0 = (uint32_t)tile.lo / kKvGroup + rec;
-    typename KvRecords<D>::Place place = records.find(rec0 + p.u0 * Z::RECS);
+    typename KvRecords<D>::Place place = records.find_later(rec0 + p.u0 * Z::RECS);
     Raw<D> raw;
     const auto load = [&](int u) {  // unit u, whose place is known; then the next one's place
+      place.page = uniform_u32(place.page);
       const __amdgpu_buffer_rsrc_t r = records.at(place);
       raw.bad = records.bad(place);
       if (with_k) {
@@ -114,7 +115,7 @@ template <int D, bool BF16> __global__ __launch_bounds__(kKvThreads, 2) void k_k
         load_words<D / 32, false>(r, off.v, raw.v);
         raw.vs = __builtin_amdgcn_raw_buffer_load_b32(r, (int)off.vs, 0, 0);
       }
-      place = records.find(rec0 + (u + 1) * Z::RECS);
+      place = records.find_later(rec0 + (u + 1) * Z::RECS);
     };
     const auto put = [&](int u, int b) {
       uint8_t* to = lds[b];
@@ -149,49 +150,60 @@ template <int D, bool BF16> __global__ __launch_bounds__(kKvThreads, 2) void k_k
         put(u + 1, b ^ 1);
         load(u + 2);
       }
+      const int tok = tile.lo + u * Z::UNIT;
+      if (tok <= last && (a.window <= 0 || tok + Z::UNIT - 1 > first - a.window)) {  // (else none of the wave's rows sees them)
+        const bf16x8* ko = reinterpret_cast<const bf16x8*>(lds[b]) + lane;
+        const f16x8* vo = reinterpret_cast<const f16x8*>(lds[b] + Z::KOPS * 1024) + lane;
+        f32x4 z[QT][Z::RECS];
 #pragma unroll
-      for (int pair = 0; pair < Z::RECS / 2; ++pair) {
-        const int tok = tile.lo + u * Z::UNIT + pair * 32;
-        if (tok > last || (a.window > 0 && tok + 31 <= first - a.window)) continue;  // none of the wave's rows sees them
-        const bf16x8* ko = reinterpret_cast<const bf16x8*>(lds[b]) + pair * 2 * (D / 32) * 64 + lane;
-        const f16x8* vo = reinterpret_cast<const f16x8*>(lds[b] + Z::KOPS * 1024) + pair * (D / 16) * 64 + lane;
-        f32x4 z[QT][2];
+        for (int t = 0; t < QT; ++t)
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
+          for (int s = 0; s < Z::RECS; ++s) z[t][s] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-          for (int t = 0; t < QT; ++t) z[t][s] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int s0 = 0; s0 < Z::RECS; s0 += 2)
 #pragma unroll
-          for (int j = 0; j < D / 32; ++j) {
-            const bf16x8 k = ko[(s * (D / 32) + j) * 64];
+          for (int j = 0; j < D / 32; ++j)
 #pragma unroll
-            for (int n = Z::NQ - 1; n >= 0; --n)
+            for (int s = s0; s < s0 + 2; ++s) {
+              const bf16x8 k = ko[(s * (D / 32) + j) * 64];
 #pragma unroll
-              for (int t = 0; t < QT; ++t) z[t][s] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, q[t][n][j], z[t][s], 0, 0, 0);
+              for (int n = Z::NQ - 1; n >= 0; --n)
+#pragma unroll
+                for (int t = 0; t < QT; ++t) z[t][s] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, q[t][n][j], z[t][s], 0, 0, 0);
+            }
+        __builtin_amdgcn_s_setprio(1);  // (the other wave's products need no issue while they run)
+        uint32_t odd = 0;
+#pragma unroll
+        for (int s = 0; s < Z::RECS; ++s) odd |= wide[b][s];
+        weights<D, QT, Z::RECS>(w, a, z, tok, !(tok + Z::UNIT - 1 <= first && (a.window <= 0 || tok > last - a.window)));
+#pragma unroll
+        for (int s0 = 0; s0 < Z::RECS; s0 += 2) {
+          f16x8 part[QT][Z::NP];
+          weight_operands<QT, Z::NP, Z::RECS>(z, s0, part);
+#pragma unroll
+          for (int j = 0; j < D / 16; ++j) {
+            const f16x8 v = vo[(s0 / 2 * (D / 16) + j) * 64];
+#pragma unroll
+            for (int n = Z::NP - 1; n >= 0; --n)
+#pragma unroll
+              for (int t = 0; t < QT; ++t) w.o[t][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, part[t][n], w.o[t][j], 0, 0, 0);
           }
         }
-        const bool odd = uniform_u32(wide[b][2 * pair] | wide[b][2 * pair + 1]) != 0;
-        weights<D, QT>(w, a, z, tok, !(tok + 31 <= first && (a.window <= 0 || tok > last - a.window)));
-        if (__builtin_expect(odd, 0)) {
+        __builtin_amdgcn_s_setprio(0);
+        if (__builtin_expect(uniform_u32(odd) != 0, 0)) {
           asm volatile("");
-          uint32_t v[2][D / 32], vs[2];
 #pragma unroll
-          for (int s = 0; s < 2; ++s) {
-            const __amdgpu_buffer_rsrc_t r = records.at(records.find((uint32_t)tok / kKvGroup + s));
-            load_words<D / 32, false>(r, off.v, v[s]);
-            vs[s] = hidden_as_one(__builtin_amdgcn_raw_buffer_load_b32(r, (int)off.vs, 0, 0), tok + 16 * s + 4 * g, tile.hi);
-            if (wide[b][2 * pair + s] == 0u) no_values(v[s], vs[s]);  // (its operands are in LDS)
+          for (int s0 = 0; s0 < Z::RECS; s0 += 2) {
+            uint32_t v[2][D / 32], vs[2];
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+              const __amdgpu_buffer_rsrc_t r = records.at(records.find((uint32_t)tok / kKvGroup + s0 + s));
+              load_words<D / 32, false>(r, off.v, v[s]);
+              vs[s] = hidden_as_one(__builtin_amdgcn_raw_buffer_load_b32(r, (int)off.vs, 0, 0), tok + 16 * (s0 + s) + 4 * g, tile.hi);
+              if (wide[b][s0 + s] == 0u) no_values(v[s], vs[s]);  // (its operands are in LDS)
+            }
+            wide_values<D, QT, Z::RECS>(w, a, v, vs, z, s0, tok + 16 * s0);
           }
-          wide_values<D, QT>(w, a, v, vs, z, tok);
-        }
-        f16x8 part[QT][Z::NP];
-        weight_operands<QT, Z::NP>(z, part);
-#pragma unroll
-        for (int j = 0; j < D / 16; ++j) {
-          const f16x8 v = vo[j * 64];
-#pragma unroll
-          for (int n = Z::NP - 1; n >= 0; --n)
-#pragma unroll
-            for (int t = 0; t < QT; ++t) w.o[t][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, part[t][n], w.o[t][j], 0, 0, 0);
         }
       }
       lds_barrier();

@@ -122,15 +122,15 @@ __device__ __forceinline__ void step(Wave<D, QT, BF16>& w, const KvAttentionArgs
 #pragma unroll
     for (int u = 0; u < 2; ++u) vs[u] = hidden_as_one(vs[u], tok + 16 * u + 4 * g, hi);
   }
-  weights<D, QT>(w, a, z, tok, masked);
+  weights<D, QT, 2>(w, a, z, tok, masked);
   if (__builtin_expect(__ballot((not_narrow(vs[0]) | not_narrow(vs[1])) != 0) != 0, 0)) {
     asm volatile("");
-    wide_values<D, QT>(w, a, s.v, vs, z, tok);
+    wide_values<D, QT, 2>(w, a, s.v, vs, z, 0, tok);
     no_values(s.v[0], vs[0]);
     no_values(s.v[1], vs[1]);
   }
   f16x8 part[QT][Z::NP];
-  weight_operands<QT, Z::NP>(z, part);
+  weight_operands<QT, Z::NP, 2>(z, 0, part);
   float sc[2][4];
 #pragma unroll
   for (int u = 0; u < 2; ++u)
