@@ -323,11 +323,11 @@ struct KvAttentionArgs {
   int limit;             // tokens a row of the table reaches
   float c;               // scale * log2(e)
   int window;            // 0: none
-  int tiles;             // without a plan: tiles of a sequence's query heads
+  int tiles;             // of a sequence's query heads; with q_start: of all queries, at most
   int blocks;
   // workspace
   int* head;             // plan: tiles of a head, and what they cost
-  KvPlanEntry* plan;
+  KvPlanEntry* plan;     // null: each block makes its own
   int* prefix;           // what is in front of each tile (KvRun)
   int* first;            // [B + 1] first tile of each sequence
   int parts;             // without a plan: parts of a tile that tickets join (64 KB); 0: a last kernel does

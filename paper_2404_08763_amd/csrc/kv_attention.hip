@@ -227,7 +227,7 @@ hipError_t launch_kv_attention(KvAttentionArgs a, int d, bool bf16, hipStream_t 
   a.first = reinterpret_cast<int*>(ws + sh.off_first);
   a.desc = reinterpret_cast<int4*>(ws + sh.off_desc);
   a.part = reinterpret_cast<float*>(ws + sh.off_part);
-  a.tiles = (a.hq / a.hkv + sh.R - 1) / sh.R;
+  a.tiles = a.q_start ? (int)sh.tiles : (a.hq / a.hkv + sh.R - 1) / sh.R;
   // The last block to arrive joins a tile's parts where they are 64 KB at most if all tiles are
   // as long as the tables (tiles of very different lengths: KvRun); more of them a kernel of their own.
   const int row_bytes = std::min(sh.R, a.hq / a.hkv) * d * 4;
@@ -238,7 +238,9 @@ hipError_t launch_kv_attention(KvAttentionArgs a, int d, bool bf16, hipStream_t 
   // no more blocks than units
   const double most = (double)sh.tiles * a.hkv * (double)(units_most(a, sh.unit) + sh.lead);
   a.blocks = most < sh.blocks ? ((int)most + 7) / 8 * 8 : sh.blocks;
-  if (a.q_start) {
+  if (a.q_start && sh.tiles <= (size_t)kKvOwnTiles && a.B <= kKvOwnSequences) {
+    a.plan = nullptr;  // (each block makes it: 2 us of each instead of a launch of 4)
+  } else if (a.q_start) {
     KernelTimer tm("kv_plan", s);
     const int listed = (int)sh.tiles;
 #define CATS_GO(U, L) \

@@ -103,6 +103,45 @@ __device__ __forceinline__ uint32_t quotient(uint64_t n, uint32_t d) {
   return (n >> 32) == 0 ? (uint32_t)n / d : (uint32_t)(n / d);
 }
 
+// The tiles of ragged queries, made by each block for itself where they are few (a.plan is null).
+constexpr int kKvOwnTiles = 1024, kKvOwnSequences = kKvThreads;
+struct KvOwnPlan {
+  int prefix[kKvOwnTiles];     // what is in front of each tile
+  int first[kKvOwnSequences];  // first tile of each sequence
+  uint16_t seq[kKvOwnTiles];
+};
+template <int UNIT, int LEAD, int R>
+__device__ __forceinline__ int kv_own_plan(const KvAttentionArgs& a, KvOwnPlan& own, uint32_t& W, int* sh) {
+  const int G = a.hq / a.hkv, me = threadIdx.x;
+  int start, n = 0, tiles;
+  if (me < a.B) n = (kv_queries(a, me, start) * G + R - 1) / R;
+  own.first[me] = block_prefix<kKvThreads>(n, tiles, sh);
+  tiles = min(tiles, a.tiles);  // (there are more only where q_start decreases)
+  __syncthreads();
+  W = 0;
+  for (int base = 0; base < tiles; base += kKvThreads) {
+    const int e = base + me;
+    int u = 0, total, lo = 0;
+    if (e < tiles) {
+      int left = a.B;  // the last sequence with first[b] <= e: it has tiles
+      while (left > 1) {
+        const int half = left / 2;
+        if (own.first[lo + half] <= e) lo += half, left -= half;
+        else left = half;
+      }
+      u = kv_tile<UNIT>(a, G, lo, (e - own.first[lo]) * R, R, kv_length(a, lo)).units + LEAD;
+    }
+    const int at = block_prefix<kKvThreads>(u, total, sh);
+    if (e < tiles) {
+      own.prefix[e] = (int)W + at;
+      own.seq[e] = (uint16_t)lo;
+    }
+    W += (uint32_t)total;
+  }
+  __syncthreads();
+  return tiles;
+}
+
 // A block's share.  The tiles of a head lie one behind the other, the heads behind each other,
 // each tile as its units and LEAD more, which stand for what a tile costs besides; each
 // block has a run of that line, all of one length but for one, whatever the sequences' lengths.
@@ -118,9 +157,9 @@ struct KvRun {
 };
 
 template <bool PLAN, int UNIT, int LEAD, int R>
-__device__ __forceinline__ bool kv_run(const KvAttentionArgs& a, KvRun& r, int* sh) {
+__device__ __forceinline__ bool kv_run(const KvAttentionArgs& a, KvRun& r, int* sh, KvOwnPlan* own = nullptr) {
   const int G = a.hq / a.hkv;
-  r.tiles = PLAN ? a.head[0] : a.tiles;
+  r.tiles = a.tiles;
   int len = 0;
   const auto cost = [&](int b) {
     if (b >= a.B) return 0;
@@ -131,7 +170,12 @@ __device__ __forceinline__ bool kv_run(const KvAttentionArgs& a, KvRun& r, int* 
   uint32_t W = 0;  // of a head
   int mine = 0, before = 0, top = 0;
   if constexpr (PLAN) {
-    W = (uint32_t)a.head[1];
+    if (a.plan) {
+      r.tiles = a.head[0];
+      W = (uint32_t)a.head[1];
+    } else {
+      r.tiles = kv_own_plan<UNIT, LEAD, R>(a, *own, W, sh);
+    }
   } else {
     for (int base = 0; base < a.B; base += kKvThreads) {
       int total;
@@ -163,13 +207,14 @@ __device__ __forceinline__ bool kv_run(const KvAttentionArgs& a, KvRun& r, int* 
     int lo = 0, n = r.tiles;  // the last tile whose prefix is not behind x
     while (n > 1) {
       const int stride = (n + kKvThreads - 1) / kKvThreads, at = threadIdx.x * stride;
-      const int last = (int)uniform_u32(__syncthreads_count(at < n && (uint32_t)a.prefix[lo + at] <= x)) - 1;
+      const bool before_x = at < n && (uint32_t)(a.plan ? a.prefix[lo + at] : own->prefix[lo + at]) <= x;
+      const int last = (int)uniform_u32(__syncthreads_count(before_x)) - 1;
       lo += last * stride;
       n = min(stride, n - last * stride);
     }
     r.e = lo;
     r.b = 0;
-    r.skip = (int)(x - (uint32_t)a.prefix[lo]);
+    r.skip = (int)(x - (uint32_t)(a.plan ? a.prefix[lo] : own->prefix[lo]));
   } else {
     uint32_t sum = 0;
     for (int base = 0;; base += kKvThreads) {
@@ -201,9 +246,16 @@ __device__ __forceinline__ bool kv_run(const KvAttentionArgs& a, KvRun& r, int* 
 }
 
 // The run's present tile.
-template <bool PLAN, int UNIT, int R> __device__ __forceinline__ KvTile kv_tile_of(const KvAttentionArgs& a, int G, const KvRun& r) {
+template <bool PLAN, int UNIT, int R>
+__device__ __forceinline__ KvTile kv_tile_of(const KvAttentionArgs& a, int G, const KvRun& r, const KvOwnPlan* own = nullptr) {
   if constexpr (PLAN) {
-    const KvPlanEntry t = a.plan[r.e];
+    KvPlanEntry t;
+    if (a.plan) {
+      t = a.plan[r.e];
+    } else {
+      t.b = own->seq[r.e];
+      t.row0 = (r.e - own->first[t.b]) * R;
+    }
     const int b = (int)uniform_u32(t.b);
     return kv_tile<UNIT>(a, G, b, (int)uniform_u32(t.row0), R, kv_length(a, b));
   } else {

@@ -60,11 +60,12 @@ template <int D, bool BF16> __global__ __launch_bounds__(kKvThreads, 2) void k_k
   const KvLane<D> off;
   const int rec = wave % Z::RECS;  // the wave's record of a step
   const bool with_k = Z::RECS == 4 || wave < 2, with_v = Z::RECS == 4 || wave >= 2;
+  __shared__ KvOwnPlan own;
   KvRun run;
-  if (!kv_run<true, Z::UNIT, kPromptLead, R>(a, run, sh)) return;
+  if (!kv_run<true, Z::UNIT, kPromptLead, R>(a, run, sh, &own)) return;
 
   while (run.p < run.p1) {
-    const KvTile tile = kv_tile_of<true, Z::UNIT, R>(a, G, run);
+    const KvTile tile = kv_tile_of<true, Z::UNIT, R>(a, G, run, &own);
     const KvPart p = kv_part<kPromptLead>(run, tile);
     if (p.u0 >= p.u1) {
       kv_next<true, kPromptLead>(a, run, tile, p);

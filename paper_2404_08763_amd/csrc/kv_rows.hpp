@@ -222,11 +222,16 @@ __global__ __launch_bounds__(kThreads, (Sizes<D, QT, BF16>::WAVES)) void k_kv_ro
   const int wave = uniform_u32(threadIdx.x / 64), lane = threadIdx.x % 64, g = lane / 16;
   const int G = a.hq / a.hkv;
   const KvLane<D> off;
+  KvOwnPlan* own = nullptr;
+  if constexpr (PLAN) {
+    __shared__ KvOwnPlan of_block;
+    own = &of_block;
+  }
   KvRun run;
-  if (!kv_run<PLAN, kUnit, kLeadUnits, R>(a, run, sh)) return;
+  if (!kv_run<PLAN, kUnit, kLeadUnits, R>(a, run, sh, own)) return;
 
   while (run.p < run.p1) {
-    const KvTile tile = kv_tile_of<PLAN, kUnit, R>(a, G, run);
+    const KvTile tile = kv_tile_of<PLAN, kUnit, R>(a, G, run, own);
     const KvPart p = kv_part<kLeadUnits>(run, tile);
     if (p.u0 >= p.u1) {
       kv_next<PLAN, kLeadUnits>(a, run, tile, p);

@@ -255,6 +255,61 @@ def test_graph_serves_other_lengths_and_pages(counts):
         _ = (q * 2).sum()
 
 
+def test_two_graphs_share_a_workspace():
+    """Replayed in turn, one of single rows (whose parts are joined by tickets in the
+    workspace) and one ragged, with eager calls of other sizes on it between them."""
+    say("kv two graphs")
+    a = Batch([1500, 20, 700], 4, 2, 64, 16, F32, seed=60)
+    b = Batch([900, 300], 4, 2, 64, 16, F32, counts=[40, 300], seed=61)
+    c = Batch([2000], 4, 2, 64, 16, F32, seed=62)
+    ws = P.kv_attention_workspace(400, 3, 4, 2, 64)
+    sets, graphs = [], []
+    for x in (a, b, c):
+        q, cache, table, lens, start = x.device()
+        out = torch.zeros_like(q)
+        call = lambda q=q, cache=cache, table=table, lens=lens, start=start, out=out: P.kv_attention(  # noqa: E731
+            q, cache, table, lens, q_start=start, out=out, ws=ws)
+        call()
+        sets.append((call, out, x.expect()))
+    torch.cuda.synchronize()
+    for call, _, _ in sets[:2]:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            call()
+        graphs.append(g)
+    for _ in range(3):
+        for _, out, _ in sets:
+            out.fill_(5.0)
+        graphs[0].replay()
+        graphs[1].replay()
+        sets[2][0]()
+        graphs[0].replay()
+        torch.cuda.synchronize()
+        for _, out, want in sets:
+            _near(out, *want)
+
+
+@pytest.mark.parametrize("n,hq,hkv,d,chunk", [(9000, 16, 1, 64, 2250), (6000, 24, 1, 128, 1500)])
+def test_long_prompt_equals_its_chunks(n, hq, hkv, d, chunk):
+    """More tiles than a block lists for itself: the same rows in chunks, which it does."""
+    say("kv long prompt", n, hq, hkv, d)
+    g = gen(63)
+    page = 256
+    cache = P.kv_cache(-(-n // page), hkv, d, page=page)
+    k, v = (torch.randn((n, hkv, d), generator=g).cuda() for _ in range(2))
+    q = torch.randn((n, hq, d), generator=g).cuda().bfloat16()
+    P.kv_write(cache, k, v, torch.arange(n, dtype=torch.int32, device="cuda"))
+    table = torch.arange(cache.shape[0], dtype=torch.int32, device="cuda")[None]
+    i32 = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    whole = P.kv_attention(q, cache, table, i32(n), q_start=i32(0, n)).float()
+    for at in range(0, n, chunk):
+        part = P.kv_attention(q[at:at + chunk], cache, table, i32(at + chunk), q_start=i32(0, chunk)).float()
+        # each is within half a step of bf16 of its sum, and the sums within 2^-10 of the weighted
+        # magnitudes (the weights' roundings to f16, half a step each), which are 1 or so
+        bound = 2.0 ** -8 * (whole[at:at + chunk].abs() + part.abs()) + 2 * 2.0 ** -10
+        assert bool(((whole[at:at + chunk] - part).abs() <= bound).all())
+
+
 def test_two_streams():
     """Two calls at once on streams and workspaces of their own."""
     say("kv streams")
