@@ -20,7 +20,7 @@
  *    "host" host memory.  `stream` is a hipStream_t (NULL = the default
  *    stream of the current device); every device pointer must belong to the
  *    current device.
- *  - The forward, dense, pack, rmsnorm and 8-bit calls only enqueue work on
+ *  - The forward, dense, pack, rmsnorm, 8-bit and attention calls only enqueue work on
  *    `stream` (no host synchronisation, no allocation).  Outputs are valid
  *    once the stream reaches that point.  The two calibration calls
  *    synchronise `stream` because they return t on the host.
@@ -502,7 +502,7 @@ cats_status cats_kv_read(const cats_kv_cache* cache, const int32_t* slots, int32
  * sequence, with key head h / (hq / heads).
  *   q, out   dev [N x hq x d], both fp32 or both bf16; must not overlap
  *   table    dev [B x width] int32: page w of sequence b holds its tokens [w page,
- *            (w + 1) page); entries behind its length are not read
+ *            (w + 1) page); entries behind its length are not used
  *   lens     dev [B] int32: tokens of each sequence, the rows' own among them
  *            (written before); taken as within [0, width * page]
  *   q_start  dev [B + 1] int32: rows [q_start[b], q_start[b + 1]) are sequence b's
@@ -512,12 +512,16 @@ cats_status cats_kv_read(const cats_kv_cache* cache, const int32_t* slots, int32
  * left as they were.  A row that sees a token of a page outside [0, pages) becomes NaN.
  * Masked tokens have no effect, whatever the cache holds for them.
  * Products of q and the cache's values are exact and summed in fp32, as is the
- * softmax; its weights enter the second product rounded to f16 (11 bits) for bf16
- * rows, as two such parts (22 bits) for fp32 rows.  A row's bits may depend on the other sequences of the
- * call (how the keys are shared out), but not from run to run.
+ * softmax; its weights enter the second product rounded to f16 (11 bits) for
+ * bf16 rows, as two such parts (22 bits) for fp32 rows.  A row's bits may depend
+ * on the other sequences of the call (how the keys are shared out), but not from
+ * run to run.
  * Workspace: cats_kv_attention_workspace_bytes(N, B, hq, heads, d), which serves
  * every call of up to as many rows and sequences of the same heads.
- * 1 <= N, B <= CATS_MAX_KV_ROWS, hq a multiple of heads, scale > 0, window >= 0. */
+ * 1 <= N, B <= CATS_MAX_KV_ROWS, hq a multiple of heads, scale > 0, window >= 0.
+ * CATS_ERR_SHAPE also where the tiles of 16 to 128 rows times the units of 32 to
+ * 128 tokens of a table's row reach 2^31: a prompt of 2^20 rows and one query head for
+ * each key head, over a table of 2^24 tokens, say; such rows are given in several calls. */
 size_t cats_kv_attention_workspace_bytes(int32_t N, int32_t B, int32_t hq, int32_t heads, int32_t d);
 cats_status cats_kv_attention(const void* q, int32_t dtype, int32_t N, int32_t hq, const cats_kv_cache* cache,
                               const int32_t* table, int32_t width, const int32_t* lens, const int32_t* q_start, int32_t B,

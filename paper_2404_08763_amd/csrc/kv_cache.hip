@@ -6,6 +6,8 @@
 // together while their lines are in the L2.  The codes come from the conversion
 // instructions: nearest value, ties to even, largest 6, scales powers of two, so
 // nothing is rounded but the value to its code.
+#include <algorithm>
+
 #include "internal.hpp"
 #include "kv4.hpp"
 
@@ -130,19 +132,36 @@ template <int D, bool BF16> __global__ __launch_bounds__(kThreads) void k_kv_rea
   store8<BF16>(a.v_out, at, vw, vs);
 }
 
-template <int D> hipError_t go(bool write, bool bf16, const KvRowsArgs& a, hipStream_t s) {
-  const dim3 grid((uint32_t)((a.rows + kThreads / (D / 8) - 1) / (kThreads / (D / 8))) * a.heads);
-  KernelTimer tm(write ? "kv_write" : "kv_read", s);
+// A launch holds 2^31 threads; calls of more rows take several.
+template <int D> hipError_t go(bool write, bool bf16, KvRowsArgs a, hipStream_t s) {
+  constexpr int RB = kThreads / (D / 8);  // rows of a block
+  const int all = a.rows, most = (int)std::min<int64_t>(all, (int64_t)((1u << 31) / kThreads / a.heads) * RB);
+  const size_t elem = bf16 ? 2 : 4;
+  for (int at = 0; at < all; at += most) {
+    a.rows = std::min(most, all - at);
+    const dim3 grid((uint32_t)((a.rows + RB - 1) / RB) * a.heads);
+    KernelTimer tm(write ? "kv_write" : "kv_read", s);
 #define CATS_GO(K) hipExtLaunchKernelGGL((K), grid, dim3(kThreads), 0, s, tm.start(), tm.stop(), 0, a)
-  if (write) {
-    if (bf16) CATS_GO((k_kv_write<D, true>));
-    else CATS_GO((k_kv_write<D, false>));
-  } else {
-    if (bf16) CATS_GO((k_kv_read<D, true>));
-    else CATS_GO((k_kv_read<D, false>));
-  }
+    if (write) {
+      if (bf16) CATS_GO((k_kv_write<D, true>));
+      else CATS_GO((k_kv_write<D, false>));
+    } else {
+      if (bf16) CATS_GO((k_kv_read<D, true>));
+      else CATS_GO((k_kv_read<D, false>));
+    }
 #undef CATS_GO
-  return hipGetLastError();
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    a.slots += a.rows;
+    if (write) {
+      a.k = static_cast<const uint8_t*>(a.k) + a.rows * a.ldk * elem;
+      a.v = static_cast<const uint8_t*>(a.v) + a.rows * a.ldv * elem;
+    } else {
+      a.k_out = static_cast<uint8_t*>(a.k_out) + (size_t)a.rows * a.heads * D * elem;
+      a.v_out = static_cast<uint8_t*>(a.v_out) + (size_t)a.rows * a.heads * D * elem;
+    }
+  }
+  return hipSuccess;
 }
 
 }  // namespace

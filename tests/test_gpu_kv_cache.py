@@ -113,6 +113,29 @@ def test_cache_beyond_32_bits():
     assert torch.equal(rk.cpu().double(), held(v)) and torch.equal(rv.cpu().double(), held(k))
 
 
+def test_more_threads_than_a_launch_holds():
+    """2^31 and more: rows of no slot but for some at either end."""
+    n, heads, d = 1 << 20, 264, 64
+    if torch.cuda.mem_get_info()[0] < 160 << 30:
+        pytest.skip("needs 160 GB")
+    say("kv many rows")
+    x = torch.empty((n, heads, d), device="cuda", dtype=BF16)
+    some = torch.cat([torch.arange(5), torch.arange(n - 70, n)])
+    k = _rows(len(some), heads, d, BF16, 40)
+    x[some.cuda()] = k.cuda()
+    slots = torch.full((n,), -1, dtype=torch.int32)
+    slots[some] = torch.arange(len(some), dtype=torch.int32) + 2
+    cpu = garbage(5, heads, d, 16)
+    cache = cpu.cuda()
+    P.kv_write(cache, x, x, slots.cuda())
+    put(cpu, slots[some], k, k)
+    assert torch.equal(cache.cpu(), cpu)
+    del x
+    rk, rv = P.kv_read(cache, slots.cuda(), dtype=BF16)
+    for r in (rk, rv):
+        assert torch.equal(r[some.cuda()].cpu().double(), held(k))
+
+
 def test_graph_and_streams():
     """Captured once, replayed on other rows and slots; and on a stream of the caller's."""
     n, heads, d, page = 9, 2, 128, 16
