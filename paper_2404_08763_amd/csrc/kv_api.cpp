@@ -220,7 +220,8 @@ cats_status cats_kv_attention(const void* q, int32_t dtype, int32_t N, int32_t h
   if (!q_start && N != B) return fail(CATS_ERR_SHAPE, "without q_start N=%d must be B=%d", (int)N, (int)B);
   if (width < 1 || (int64_t)width * cache->page > CATS_MAX_KV_TOKENS)
     return fail(CATS_ERR_SHAPE, "width=%d pages of %d tokens must hold 1 to 2^30", (int)width, (int)cache->page);
-  if (!std::isfinite(scale) || !(scale > 0.f)) return fail(CATS_ERR_RANGE, "scale must be finite and > 0");
+  const float c = scale * 1.44269504088896340736f;
+  if (!std::isfinite(c) || !(scale > 0.f)) return fail(CATS_ERR_RANGE, "scale must be finite (log2(e) times it too) and > 0");
   if (window < 0) return fail(CATS_ERR_RANGE, "window=%d must be >= 0", (int)window);
   if (!aligned(q, 16) || !aligned(out, 16) || !aligned(table, 4) || !aligned(lens, 4) || !aligned(q_start, 4))
     return fail(CATS_ERR_ALIGN, "q and out must be 16-byte aligned, table, lens and q_start 4-byte");
@@ -253,7 +254,7 @@ cats_status cats_kv_attention(const void* q, int32_t dtype, int32_t N, int32_t h
   a.groups = cache->page / 16;
   a.magic = magic_of(a.groups);
   a.limit = width * cache->page;
-  a.c = scale * 1.44269504088896340736f;
+  a.c = c;
   a.window = window;
   a.head = static_cast<int*>(ws);
   if (!cats::kv_attention_fits(a, cache->d, dtype == CATS_BF16))

@@ -13,7 +13,8 @@ constexpr float kLow = -3.402823466e+38f;  // maximum of a row that has seen no 
 // score is kLazy above that, so that O is rarely multiplied: p is 2^15 at most, and f16's
 // least number 2^-31 of the largest.
 constexpr float kLead = 7.f, kLazy = 8.f;
-
+// Up to here a maximum is off by half at most: the exponents, which are exact, stay below 16.
+constexpr float kFar = 8388608.f;
 
 // ---- the work of a call -------------------------------------------------------------
 
@@ -516,6 +517,8 @@ template <int D, int QT> struct KvSums {
   f32x4 o[QT][D / 16];  // o[t][j][i]: row lane % 16, column g D/4 + i D/16 + j
   float m[QT], l[QT];   // what the exponents are counted from, the lane's part of the sum
   int pos[QT];          // the row's position, -1 and less: sees nothing
+  bool far;             // some row's m is beyond kFar; then c is 1 and off 0, else a.c and m
+  float c, off[QT];
 };
 
 // The softmax of a step: scores z of the tokens of U records from tok on become weights, the
@@ -545,6 +548,7 @@ __device__ __forceinline__ void weights(KvSums<D, QT>& w, const KvAttentionArgs&
   }
   if (__builtin_expect(__ballot(rise) != 0, 0)) {
     asm volatile("");
+    bool far = false;
 #pragma unroll
     for (int t = 0; t < QT; ++t) {
       float x = fmaxf(top[t], __shfl_xor(top[t], 16));
@@ -552,16 +556,33 @@ __device__ __forceinline__ void weights(KvSums<D, QT>& w, const KvAttentionArgs&
       const float m = fmaxf(w.m[t], x - kLead), f = __builtin_amdgcn_exp2f(w.m[t] - m);
       w.m[t] = m;
       w.l[t] *= f;
+      far |= fabsf(m) > kFar && m != kLow;
 #pragma unroll
       for (int j = 0; j < D / 16; ++j) w.o[t][j] *= f;
     }
+    w.far = __ballot(far) != 0;
+    w.c = w.far ? 1.f : a.c;
+#pragma unroll
+    for (int t = 0; t < QT; ++t) w.off[t] = w.far ? 0.f : w.m[t];
+  }
+  if (__builtin_expect(w.far, 0)) {  // the exponents of rounded products, not of exact ones
+    asm volatile("");
+#pragma unroll
+    for (int t = 0; t < QT; ++t)
+#pragma unroll
+      for (int i = 0; i < 4 * U; ++i) {
+        float x = z[t][i / 4][i % 4] * a.c;
+        asm volatile("" : "+v"(x));  // (no fused operation)
+        x -= w.m[t];
+        z[t][i / 4][i % 4] = x > kLead + kLazy ? kLead + kLazy : x;
+      }
   }
 #pragma unroll
   for (int t = 0; t < QT; ++t) {
     float l = 0.f;
 #pragma unroll
     for (int i = 0; i < 4 * U; ++i) {
-      z[t][i / 4][i % 4] = __builtin_amdgcn_exp2f(fmaf(z[t][i / 4][i % 4], a.c, -w.m[t]));
+      z[t][i / 4][i % 4] = __builtin_amdgcn_exp2f(fmaf(z[t][i / 4][i % 4], w.c, -w.off[t]));
       l += z[t][i / 4][i % 4];
     }
     w.l[t] += l;

@@ -75,6 +75,8 @@ template <int D, bool BF16> __global__ __launch_bounds__(kKvThreads, 2) void k_k
 
     // the wave's rows
     KvSums<D, QT> w;
+    w.far = false;
+    w.c = a.c;
     bf16x8 q[QT][Z::NQ][D / 32];
     const int mine = wave * 16 * QT;
 #pragma unroll
@@ -82,7 +84,7 @@ template <int D, bool BF16> __global__ __launch_bounds__(kKvThreads, 2) void k_k
       const int r = min(mine + t * 16 + lane % 16, tile.rows - 1);  // (rows behind the last repeat it and are not stored)
       const int i = (tile.row0 + r) / G, head = h * G + (tile.row0 + r) % G;
       w.pos[t] = tile.len - tile.nq + i;
-      w.m[t] = kLow;
+      w.m[t] = w.off[t] = kLow;
       w.l[t] = 0.f;
       const size_t at = ((size_t)(tile.start + i) * a.hq + head) * D + g * (D / 4);
 #pragma unroll

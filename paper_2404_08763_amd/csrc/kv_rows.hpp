@@ -51,12 +51,14 @@ template <int D, int QT, bool BF16>
 __device__ __forceinline__ void load_q(Wave<D, QT, BF16>& w, const KvAttentionArgs& a, int h, const KvTile& tile, bf16x8* sq) {
   typedef Sizes<D, QT, BF16> Z;
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, g = lane / 16, G = a.hq / a.hkv;
+  w.far = false;
+  w.c = a.c;
 #pragma unroll
   for (int t = 0; t < QT; ++t) {
     const int r = min(t * 16 + lane % 16, tile.rows - 1);  // (rows behind the last repeat it and are not stored)
     const int i = (tile.row0 + r) / G, head = h * G + (tile.row0 + r) % G;
     w.pos[t] = tile.len - tile.nq + i;
-    w.m[t] = kLow;
+    w.m[t] = w.off[t] = kLow;
     w.l[t] = 0.f;
     const size_t at = ((size_t)(tile.start + i) * a.hq + head) * D + g * (D / 4);
     if constexpr (Z::QLDS) {

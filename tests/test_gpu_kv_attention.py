@@ -7,7 +7,7 @@ import torch
 import paper_2404_08763_amd as P
 
 from gpu_util import say
-from kv_util import BF16, F32, Batch, garbage, gen
+from kv_util import BF16, F32, HALF, Batch, attention, garbage, gen
 
 pytestmark = pytest.mark.gpu
 IDS = {F32: "f32", BF16: "bf16"}
@@ -87,6 +87,28 @@ def test_scale_and_peaks(dtype):
     b = Batch([500], 2, 1, 64, 32, dtype, seed=14)
     b.q *= 0  # equal weights
     _check(b)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=IDS.get)
+@pytest.mark.parametrize("counts", [None, [1, 2, 130, 40, 3]])
+@pytest.mark.parametrize("power", [18, 24, 25, 27, 31, 45, 90])
+def test_scores_of_any_size(power, counts, dtype):
+    """q has one column, so that the scores are exact, and so far apart that the largest ones
+    alone count (a weight each): beyond 2^23, where half a step of a maximum is an exponent's error."""
+    say("kv far scores", power, counts, dtype)
+    lens = [1, 3, 200, 500, 5000]
+    b = Batch(lens, 4, 2, 64, 16, dtype, counts=counts, seed=70 + power)
+    g = gen(power)
+    col = torch.randint(0, 64, b.q.shape[:2], generator=g)
+    sign = torch.randint(0, 2, b.q.shape[:2], generator=g) * 2.0 - 1.0
+    b.q = (torch.nn.functional.one_hot(col, 64) * sign[..., None] * 2.0 ** power).to(dtype)
+    q, cache, table, start_lens, start = b.device()
+    got = P.kv_attention(q, cache, table, start_lens, q_start=start, scale=1.0).cpu().double()
+    want, _ = b.expect(scale=1.0)
+    mag, _ = attention(b.q, b.k, [v.abs() for v in b.v], b.lens, b.q_start, 0, 1.0)
+    # as attention()'s bound, without the scores' errors: equal scores have equal weights
+    rel = (2.0 ** -11 if dtype is BF16 else 2.0 ** -22) + 2.0 ** -21 + 2 * 5064 * 2.0 ** -24
+    _near(got, want, rel * mag + HALF[dtype] * want.abs())
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16], ids=IDS.get)

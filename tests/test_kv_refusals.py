@@ -122,7 +122,7 @@ def test_attention_arguments():
                 dict(hq=1032), dict(width=0), dict(width=(1 << 24) + 1)):
         assert _attn(**bad) == SHAPE, bad
     assert _attn(N=5, start=A + 6 * G, ws=0) == WORKSPACE  # (any N with q_start)
-    for scale in (0.0, -1.0, float("nan"), float("inf")):
+    for scale in (0.0, -1.0, float("nan"), float("inf"), 3e38):
         assert _attn(scale=scale) == RANGE
     assert _attn(window=-1) == RANGE
     for name, at in (("q", A + G), ("out", A + 4 * G)):
@@ -140,6 +140,13 @@ def test_attention_workspace_and_overlaps():
         assert _attn(ws=at, nbytes=need) == RANGE, at
     assert _attn(ws=A + 4 * G + 0x100, nbytes=need) == RANGE
     assert _attn(start=A + 6 * G, ws=A + 6 * G) == RANGE and _attn(start=A + 4 * G) == RANGE
+
+
+def test_attention_work_beyond_32_bits():
+    """512 tiles of 128 rows, of 2^24 units of 64 tokens each: 2^33."""
+    kw = dict(N=1 << 16, B=1, hq=8, start=A + 6 * G, nbytes=1 << 35)
+    assert _attn(width=1 << 24, **kw) == SHAPE
+    assert b"too many for one call" in P.raw().cats_last_error()
 
 
 @pytest.mark.parametrize("planned", [False, True])
