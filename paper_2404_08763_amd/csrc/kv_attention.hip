@@ -2,7 +2,7 @@
 //
 // One pass over the keys with a running maximum and sum.  A wave has a tile of
 // 16 QT rows (the query heads of a key head side by side, then the next query)
-// and takes 32 tokens a step; everything stays in its registers:
+// and takes 32 or 64 tokens a step; its sums stay in registers:
 //   - S^T = K Q^T: the records' layout (kv4.hpp) gives each lane its part of the
 //     matrix operand in one load; the conversion instructions make bf16 of the
 //     codes and scales, exactly, so the products are exact and their sums fp32.
@@ -18,8 +18,8 @@
 //
 // One kernel takes few rows of each sequence (kv_rows.hpp), another many (kv_prompt.hpp).
 // The blocks share all of a call's keys evenly, whatever the sequences' lengths (KvRun): what
-// is split over blocks is joined by a last kernel, and where the queries are ragged a first
-// one lists their tiles.
+// is split over blocks is joined by a last kernel (few rows in few parts: by the block that
+// arrives last), and where ragged queries make many tiles a first one lists them.
 #include <algorithm>
 
 #include "kv_attention.hpp"

@@ -320,7 +320,6 @@ __device__ __forceinline__ void kv_next(const KvAttentionArgs& a, KvRun& r, cons
 
 // ---- the cache's records ----------------------------------------------------------------
 
-typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
 // Words that no kernel of the call writes, at an address equal on all lanes: a scalar load.
