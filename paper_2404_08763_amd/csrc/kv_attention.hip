@@ -169,7 +169,7 @@ Shape shape_of(int N, int B, int hq, int hkv, int d, bool bf16, bool planned) {
   s.off_prefix = s.off_plan + up256(listed * sizeof(KvPlanEntry));
   s.off_first = s.off_prefix + up256(listed * 4);
   s.off_desc = s.off_first + (planned ? up256((size_t)(B + 1) * 4) : 0);
-  s.off_part = s.off_desc + up256((size_t)s.blocks * 16);
+  s.off_part = s.off_desc + up256((size_t)s.blocks * (s.prompt ? 40 : 16));
   s.bytes = s.off_part + part_bytes(d, s.R, s.blocks);
   return s;
 }
@@ -210,7 +210,7 @@ size_t kv_attention_most(int N, int B, int hq, int hkv, int d) {
   size_t part = 0;
   for (int qt = 1; qt <= 2; ++qt) part = std::max(part, part_bytes(d, 16 * qt, 256 * kv_rows_waves(d, qt)));
   part = std::max(part, part_bytes(d, kv_prompt_rows(d, true), prompt_blocks(d)));
-  return 256 + up256(tiles * sizeof(KvPlanEntry)) + up256(tiles * 4) + up256((size_t)(B + 1) * 4) + up256(kMostBlocks * 16) + part;
+  return 256 + up256(tiles * sizeof(KvPlanEntry)) + up256(tiles * 4) + up256((size_t)(B + 1) * 4) + up256(kMostBlocks * 40) + part;
 }
 
 // (the prefixes of a head's tiles are 32-bit numbers)
@@ -233,6 +233,10 @@ hipError_t launch_kv_attention(KvAttentionArgs a, int d, bool bf16, hipStream_t 
   const int row_bytes = std::min(sh.R, a.hq / a.hkv) * d * 4;
   const long long split_in = std::min<long long>(units_most(a, sh.unit), sh.blocks / ((long long)sh.tiles * a.hkv) + 2);
   a.parts = !a.q_start && split_in * row_bytes <= (64 << 10) ? (64 << 10) / row_bytes : 0;
+  // So do the blocks of a prompt with a tile for every other block or more, whose tiles are in
+  // three parts or less (1024 tiles for 480 blocks 186 us instead of 195, 256 tiles 37 instead of
+  // 44; 188 tiles 49 instead of 45, 128 tiles 33 instead of 32).
+  if (sh.prompt && (long long)a.N * (a.hq / a.hkv) / sh.R * a.hkv >= sh.blocks / 2) a.parts = 1;
   a.tickets = reinterpret_cast<unsigned long long*>(a.desc);
   a.epoch = call_epoch();
   // no more blocks than units

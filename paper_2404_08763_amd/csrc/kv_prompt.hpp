@@ -7,10 +7,11 @@
 // is multiplied (two buffers, one barrier a step).  Bound by issue: matrix cores work 0.32, vector ALUs (softmax,
 // the weights' rounding, the conversion) 0.47 of a busy compute unit's cycles, and the two waves
 // of a SIMD hide only a part of one behind the other.  4096 rows of one sequence, 32 heads of
-// 128 columns on 8 (137 GFLOP): 187 us, 0.73 PFLOP/s, with the parts' join 200.
+// 128 columns on 8 (137 GFLOP): 185 us, 0.74 PFLOP/s.
 #pragma once
 
 #include "kv_attention.hpp"
+#include "ticket.hpp"
 
 namespace cats {
 namespace {
@@ -49,6 +50,104 @@ __device__ __forceinline__ void lds_barrier() {
   __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
   __builtin_amdgcn_s_barrier();
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
+// A block's part of a sum that n blocks from `first` on share, its own the idx-th.  True where
+// the whole sum is in w: in the block that arrives last.  Four parts side by side are joined by the
+// last of their blocks, which has its own in registers, and four such sums again: the other
+// blocks write theirs and go on.  Parts are added in their order, whoever does it.  A block's last
+// tile is the next one's first, which is done long before: the part is mostly not written at all.
+constexpr int kJoin = 4;
+static_assert(kJoin * kJoin * kJoin * kJoin * kJoin >= 512, "five words of tickets for each block");
+template <int D, bool BF16>
+__device__ __forceinline__ bool join_prompt(const KvAttentionArgs& a, KvSums<D, kv_prompt_qt(D, BF16)>& w, int first, int idx, int n,
+                                            int rows, int* sh) {
+  typedef PromptSizes<D, BF16> Z;
+  constexpr int QT = Z::QT, J = D / 16;
+  int me = threadIdx.x;
+  asm volatile("" : "+v"(me));  // (nothing of this is computed in front of the loop and kept over it)
+  const int lane = me % 64, mine = me / 64 * 16 * QT;
+  const __amdgpu_buffer_rsrc_t parts = make_rsrc(a.part, (uint32_t)a.blocks * 2 * (Z::PART * 4));
+  const auto slot = [&](int i) { return (uint32_t)(2 * (first + i) + (i == 0 ? 1 : 0)) * (Z::PART * 4); };
+  // a thread's words of a part: its sums, then m and l
+  const auto word = [&](int t, int j) { return (uint32_t)((t * J + j) * kKvThreads + me) * 16; };
+  const auto stat = [&](int t) { return (uint32_t)(Z::R * D + mine + t * 16 + lane % 16) * 4; };
+  int level = 0;
+  for (int stride = 1;; stride *= kJoin, ++level) {
+    const int base = idx / (stride * kJoin) * (stride * kJoin), count = min(kJoin, (n - base + stride - 1) / stride);
+    if (count > 1) {
+      unsigned long long* ticket = a.tickets + level * a.blocks + first + base;
+      unsigned long long peek = 0;
+      if (threadIdx.x == 0) {
+        peek = ticket_peek(ticket);
+        sh[10] = peek == ((unsigned long long)a.epoch << 32 | (uint32_t)(count - 1)) ? 1 : 0;
+      }
+      __syncthreads();
+      const bool alone = sh[10] != 0;  // (the others have written theirs)
+      if (!alone) {
+        const uint32_t to = slot(idx);
+#pragma unroll
+        for (int t = 0; t < QT; ++t) {
+          if (mine + t * 16 + lane % 16 >= rows) continue;
+#pragma unroll
+          for (int j = 0; j < J; ++j) st_buf16_coherent(parts, to + word(t, j), __builtin_bit_cast(u32x4, w.o[t][j]));
+          if (lane < 16) {
+            __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(w.m[t]), parts, (int)(to + stat(t)), 0, kCachePolicySc1);
+            __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(w.l[t]), parts, (int)(to + stat(t) + Z::R * 4), 0, kCachePolicySc1);
+          }
+        }
+        __builtin_amdgcn_s_waitcnt(0);  // this thread's stores have completed
+      }
+      __syncthreads();
+      if (threadIdx.x == 0) sh[11] = take_ticket(ticket, a.epoch, (uint32_t)count, peek) ? 1 : 0;
+      __syncthreads();
+      if (sh[11] == 0) return false;
+      // (a part that is not there, and the block's own, reads as zeros)
+      uint32_t from[kJoin];
+      int own = 0;
+#pragma unroll
+      for (int k = 0; k < kJoin; ++k) {
+        const int i = base + k * stride;
+        own = i == idx ? k : own;
+        from[k] = k < count && i != idx ? slot(i) : kOOB;
+      }
+#pragma unroll
+      for (int t = 0; t < QT; ++t) {
+        float f[kJoin], l[kJoin], top = w.m[t];
+#pragma unroll
+        for (int k = 0; k < kJoin; ++k) {
+          f[k] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(parts, (int)(from[k] + stat(t)), 0, kCachePolicySc1));
+          l[k] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(parts, (int)(from[k] + stat(t) + Z::R * 4), 0, kCachePolicySc1));
+        }
+#pragma unroll
+        for (int k = 0; k < kJoin; ++k) {
+          f[k] = k == own ? w.m[t] : k < count ? f[k] : kLow;
+          l[k] = k == own ? w.l[t] : l[k];
+          top = fmaxf(top, f[k]);
+        }
+        float sum = 0.f;
+#pragma unroll
+        for (int k = 0; k < kJoin; ++k) {
+          f[k] = __builtin_amdgcn_exp2f(f[k] - top);
+          sum += l[k] * f[k];
+        }
+        w.m[t] = top;
+        w.l[t] = sum;
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+          f32x4 po[kJoin], o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int k = 0; k < kJoin; ++k) po[k] = __builtin_bit_cast(f32x4, ld_buf16_coherent(parts, from[k] + word(t, j)));
+#pragma unroll
+          for (int k = 0; k < kJoin; ++k) o += (k == own ? w.o[t][j] : po[k]) * f[k];
+          w.o[t][j] = o;
+          if (j % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+        }
+      }
+    }
+    idx = base;
+    if (stride * kJoin >= n) return true;
+  }
 }
 
 template <int D, bool BF16> __global__ __launch_bounds__(kKvThreads, 2) void k_kv_prompt(KvAttentionArgs a) {
@@ -214,33 +313,44 @@ template <int D, bool BF16> __global__ __launch_bounds__(kKvThreads, 2) void k_k
       lds_barrier();
     }
 
-    float* part = a.part + ((size_t)run.lb * 2 + (p.head ? 1 : 0)) * Z::PART;
 #pragma unroll
     for (int t = 0; t < QT; ++t) {
-      float l = w.l[t];
-      l += __shfl_xor(l, 16);
-      l += __shfl_xor(l, 32);
+      w.l[t] += __shfl_xor(w.l[t], 16);
+      w.l[t] += __shfl_xor(w.l[t], 32);
+    }
+    if (!p.whole && a.parts > 0) {
+      int n;
+      const int first_block = kv_parts_of<kPromptLead>(run, tile, p, n);
+      if (!join_prompt<D, BF16>(a, w, first_block, run.lb - first_block, n, tile.rows, sh)) {
+        kv_next<true, kPromptLead>(a, run, tile, p);
+        continue;
+      }
+    }
+#pragma unroll
+    for (int t = 0; t < QT; ++t) {
       const int r = mine + t * 16 + lane % 16;
       if (r >= tile.rows) continue;
       const int i = (tile.row0 + r) / G;
       const bool empty = w.pos[t] < 0;  // sees no key: zeros
       const size_t at = ((size_t)(tile.start + i) * a.hq + h * G + (tile.row0 + r) % G) * D + g * (D / 4);
-      const float inv = p.whole ? 1.f / l : 1.f;
+      float* part = a.part + ((size_t)run.lb * 2 + (p.head ? 1 : 0)) * Z::PART;
+      const bool last_kernel = !p.whole && a.parts == 0;  // joins the parts
+      const float inv = last_kernel ? 1.f : 1.f / w.l[t];
 #pragma unroll
       for (int c = 0; c < 4; ++c)
 #pragma unroll
         for (int j = 0; j < D / 16; j += 4) {
           f32x4 o = f32x4{w.o[t][j][c], w.o[t][j + 1][c], w.o[t][j + 2][c], w.o[t][j + 3][c]} * inv;
-          if (p.whole) {
+          if (last_kernel) {
+            *reinterpret_cast<f32x4*>(part + r * D + g * (D / 4) + c * (D / 16) + j) = o;
+          } else {
             if (empty) o = f32x4{0.f, 0.f, 0.f, 0.f};
             store_out<BF16>(a.out, at + c * (D / 16) + j, o);
-          } else {
-            *reinterpret_cast<f32x4*>(part + r * D + g * (D / 4) + c * (D / 16) + j) = o;
           }
         }
-      if (!p.whole && g == 0) {
+      if (last_kernel && g == 0) {
         part[R * D + r] = empty ? -__builtin_inff() : w.m[t];
-        part[R * D + R + r] = l;
+        part[R * D + R + r] = w.l[t];
       }
     }
     kv_next<true, kPromptLead>(a, run, tile, p);

@@ -332,6 +332,54 @@ def test_long_prompt_equals_its_chunks(n, hq, hkv, d, chunk):
         assert bool(((whole[at:at + chunk] - part).abs() <= bound).all())
 
 
+@pytest.mark.parametrize("dtype,d,n", [(BF16, 64, 200000), (F32, 64, 60001), (BF16, 128, 100000)])
+def test_prompt_beside_a_long_sequence(dtype, d, n):
+    """Tiles in one, two and, the long sequence's, in tens of parts, joined by the blocks that
+    have them: as calls of each sequence alone, whose parts another kernel joins.  In a graph too,
+    replayed with eager calls on its workspace in between: the same bits."""
+    say("kv skew", dtype, d, n)
+    heads, rows, page = 16, [40, 4200], 256
+    lens = [n, rows[1]]
+    g = gen(64)
+    need = [-(-x // page) for x in lens]
+    cache = P.kv_cache(sum(need), heads, d, page=page)
+    for b, x in enumerate(lens):
+        k, v = (torch.randn((x, heads, d), generator=g).cuda() for _ in range(2))
+        P.kv_write(cache, k, v, torch.arange(x, dtype=torch.int32, device="cuda") + sum(need[:b]) * page)
+    table = torch.zeros((2, max(need)), dtype=torch.int32)
+    table[0, :need[0]] = torch.arange(need[0])
+    table[1, :need[1]] = torch.arange(need[1]) + need[0]
+    table = table.cuda()
+    i32 = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    q = torch.randn((sum(rows), heads, d), generator=g).cuda().to(dtype)
+    ws = P.kv_attention_workspace(sum(rows), 2, heads, heads, d)
+    where, starts, out = i32(*lens), i32(0, rows[0], sum(rows)), torch.zeros_like(q)
+    call = lambda: P.kv_attention(q, cache, table, where, q_start=starts, out=out, ws=ws)  # noqa: E731
+    whole = call().clone()
+    # the weights' roundings on both sides, 2^-11 or 2^-22 of their sum with |v|, which is 6 at most and
+    # far less where there are many tokens; the sums of up to n terms; the output's rounding
+    cut = 2 * (2.0 ** -11 if dtype is BF16 else 2.0 ** -22 + 4000 * 2.0 ** -24)
+    for b, at in enumerate((0, rows[0])):
+        step = 40 if b == 0 else 1050
+        for i in range(0, rows[b], step):
+            part = P.kv_attention(q[at + i:at + i + step], cache, table[b:b + 1], i32(lens[b] - rows[b] + i + step),
+                                  q_start=i32(0, step), ws=ws).double()
+            mine = whole[at + i:at + i + step].double()
+            bound = HALF[dtype] * (mine.abs() + part.abs()) + 2 * cut
+            assert bool(((mine - part).abs() <= bound).all()), (b, i)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for r in range(3):
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, whole)
+        P.kv_attention(q[:40], cache, table[:1], i32(5000), q_start=i32(0, 40), ws=ws)
+        assert torch.equal(call(), whole)
+
+
 def test_two_streams():
     """Two calls at once on streams and workspaces of their own."""
     say("kv streams")
