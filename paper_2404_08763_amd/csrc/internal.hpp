@@ -333,7 +333,10 @@ struct KvAttentionArgs {
   int parts;             // without a plan: parts of a tile that tickets join (64 KB); 0: a last kernel does
   uint32_t epoch;        // the tickets' tag
   unsigned long long* tickets;  // [blocks] of the sum that begins in each block
-  int4* desc;            // [blocks] the same's place, for the last kernel
+  // for the last kernel: {parts | first block << 16, h, b, row0} of a tile, in order of the tiles
+  // where there are fewer than blocks (by_tile), else of the block that it begins in
+  int4* desc;            // [sums]
+  int sums, by_tile;
   float* part;           // [blocks x 2] partial sums
 };
 // Workspace of a call, and at most of any call of up to N rows and B sequences.

@@ -75,17 +75,17 @@ __global__ __launch_bounds__(kPlanThreads) void k_kv_plan(KvAttentionArgs a, int
 
 // ---- parts into one -----------------------------------------------------------
 
-// Joins the sum that begins in block lb: its first part there, the others in the blocks
+// Joins a sum that desc notes: its first part in block lb, the others in the blocks
 // behind it.  D / 4 threads have a row of a part.  ROW: a block has one row and takes its parts
 // side by side (few rows, many parts); else it has as many rows as it holds.
 template <int D, bool BF16, bool ROW> __global__ __launch_bounds__(kKvThreads) void k_kv_join(KvAttentionArgs a, int R) {
   constexpr int L = D / 4, S = kKvThreads / L;
   const int PART = R * (D + 2);
   const int s = threadIdx.x / L, c = threadIdx.x % L * 4;
-  const int lb = blockIdx.x, row = ROW ? blockIdx.y : blockIdx.y * S + s;
-  const int4 d = a.desc[lb];
-  if (d.x == 0) return;
-  const int n = d.x, h = d.y, b = d.z, row0 = d.w, G = a.hq / a.hkv;
+  const int row = ROW ? blockIdx.y : blockIdx.y * S + s;
+  const int4 d = a.desc[blockIdx.x];
+  const int n = d.x & 0xffff, lb = d.x >> 16, h = d.y, b = d.z, row0 = d.w, G = a.hq / a.hkv;
+  if (n == 0) return;
   int start;
   const int nq = kv_queries(a, b, start);
   if (row >= min(R, nq * G - row0)) return;
@@ -179,8 +179,8 @@ long long units_most(const KvAttentionArgs& a, int unit) { return ((long long)a.
 
 template <int D> hipError_t join(const KvAttentionArgs& a, const Shape& sh, bool bf16, hipStream_t s) {
   KernelTimer tm("kv_join", s);
-  const int at_once = sh.prompt ? kKvThreads / (D / 4) : 1;
-  const dim3 grid(a.blocks, (sh.R + at_once - 1) / at_once), th(kKvThreads);
+  const int at_once = sh.prompt ? kKvThreads / (D / 4) : 1, rows = a.q_start ? sh.R : std::min(sh.R, a.hq / a.hkv);
+  const dim3 grid(a.sums, (rows + at_once - 1) / at_once), th(kKvThreads);
 #define CATS_GO(B, ROW) hipExtLaunchKernelGGL((k_kv_join<D, B, ROW>), grid, th, 0, s, tm.start(), tm.stop(), 0, a, sh.R)
   if (bf16) {
     if (sh.prompt) CATS_GO(true, false);
@@ -242,6 +242,8 @@ hipError_t launch_kv_attention(KvAttentionArgs a, int d, bool bf16, hipStream_t 
   // no more blocks than units
   const double most = (double)sh.tiles * a.hkv * (double)(units_most(a, sh.unit) + sh.lead);
   a.blocks = most < sh.blocks ? ((int)most + 7) / 8 * 8 : sh.blocks;
+  a.by_tile = sh.tiles * a.hkv <= (size_t)a.blocks ? 1 : 0;
+  a.sums = a.by_tile ? (int)sh.tiles * a.hkv : a.blocks;
   if (a.q_start && sh.tiles <= (size_t)kKvOwnTiles && a.B <= kKvOwnSequences) {
     a.plan = nullptr;  // (each block makes it: 2 us of each instead of a launch of 4)
   } else if (a.q_start) {

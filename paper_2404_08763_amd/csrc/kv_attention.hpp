@@ -196,7 +196,12 @@ __device__ __forceinline__ bool kv_run(const KvAttentionArgs& a, KvRun& r, int* 
     if ((uint64_t)nb * one > most) nb = quotient(most, one);
   }
   r.lb = nb < (uint32_t)a.blocks ? (int)blockIdx.x : (int)((blockIdx.x % 8) * (nb / 8) + blockIdx.x / 8);
-  if (a.parts == 0 && threadIdx.x == 0) a.desc[r.lb] = int4{0, 0, 0, 0};
+  if (a.parts == 0 && a.by_tile) {  // (each tile there is notes itself)
+    for (int i = r.tiles * (PLAN ? 1 : a.B) * a.hkv + blockIdx.x * kKvThreads + threadIdx.x; i < a.sums; i += a.blocks * kKvThreads)
+      a.desc[i] = int4{0, 0, 0, 0};
+  } else if (a.parts == 0 && threadIdx.x == 0) {
+    a.desc[r.lb] = int4{0, 0, 0, 0};
+  }
   if ((uint32_t)r.lb >= nb) return false;
   r.base = quotient(T, nb);
   r.rem = (uint32_t)(T - (uint64_t)r.base * nb);
@@ -295,14 +300,15 @@ template <int LEAD> __device__ __forceinline__ int kv_parts_of(const KvRun& r, c
 }
 
 // Goes on to the next tile; before, notes for the last kernel (without tickets) a sum that
-// begins in this block and ends in a later one.
+// begins in this block and ends in a later one (by tile: any that begins here).
 template <bool PLAN, int LEAD>
 __device__ __forceinline__ void kv_next(const KvAttentionArgs& a, KvRun& r, const KvTile& t, const KvPart& p) {
   const uint64_t end = r.p - (uint32_t)r.skip + (uint32_t)(t.units + LEAD);  // of the tile, on the line
-  if (a.parts == 0 && p.head && !p.whole && threadIdx.x == 0) {
-    int n;
-    kv_parts_of<LEAD>(r, t, p, n);
-    a.desc[r.lb] = int4{n, r.h, t.b, t.row0};
+  if (a.parts == 0 && p.head && (a.by_tile || !p.whole) && threadIdx.x == 0) {
+    int n = 0;
+    if (!p.whole) kv_parts_of<LEAD>(r, t, p, n);
+    const int at = !a.by_tile ? r.lb : PLAN ? r.h * r.tiles + r.e : (r.h * a.B + r.b) * r.tiles + r.e;
+    a.desc[at] = int4{n | r.lb << 16, r.h, t.b, t.row0};
   }
   r.p = end < r.p1 ? end : r.p1;
   r.skip = 0;
