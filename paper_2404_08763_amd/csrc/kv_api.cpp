@@ -255,7 +255,7 @@ cats_status cats_kv_attention(const void* q, int32_t dtype, int32_t N, int32_t h
   a.magic = magic_of(a.groups);
   a.limit = width * cache->page;
   a.c = c;
-  a.window = window;
+  a.window = window < a.limit ? window : 0;  // (one that holds every token is none)
   a.head = static_cast<int*>(ws);
   if (!cats::kv_attention_fits(a, cache->d, dtype == CATS_BF16))
     return fail(CATS_ERR_SHAPE, "%d rows of %d sequences over tables of %d tokens are too many for one call", (int)N, (int)B, a.limit);

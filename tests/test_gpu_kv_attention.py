@@ -60,6 +60,14 @@ def test_window_of_single_rows(window, dtype):
     _check(Batch(LENS, 6, 2, 128, 32, dtype, seed=5), window=window)
 
 
+@pytest.mark.parametrize("window", [79, 80, 81, 2 ** 30, 2 ** 31 - 1])
+@pytest.mark.parametrize("counts", [[9, 80], [90, 70]])
+def test_windows_around_and_beyond_the_table(counts, window):
+    """Rows in front of a sequence's first token among them (positions down to -85)."""
+    say("kv wide window", window, counts)
+    _check(Batch([5, 80], 4, 2, 64, 16, BF16, counts=counts, seed=17), window=window)
+
+
 @pytest.mark.parametrize("dtype", [F32, BF16], ids=IDS.get)
 def test_long_sequences_are_split_and_joined(dtype):
     """One sequence over every block, and a few of very different lengths."""
