@@ -344,7 +344,7 @@ def test_long_prompt_equals_its_chunks(n, hq, hkv, d, chunk):
 def test_prompt_beside_a_long_sequence(dtype, d, n):
     """Tiles in one, two and, the long sequence's, in tens of parts, joined by the blocks that
     have them: as calls of each sequence alone, whose parts another kernel joins.  In a graph too,
-    replayed with eager calls on its workspace in between: the same bits."""
+    replayed with eager calls and rubbish on its workspace in between: the same bits."""
     say("kv skew", dtype, d, n)
     heads, rows, page = 16, [40, 4200], 256
     lens = [n, rows[1]]
@@ -385,6 +385,8 @@ def test_prompt_beside_a_long_sequence(dtype, d, n):
         torch.cuda.synchronize()
         assert torch.equal(out, whole)
         P.kv_attention(q[:40], cache, table[:1], i32(5000), q_start=i32(0, 40), ws=ws)
+        if r:
+            ws.random_(0, 256)
         assert torch.equal(call(), whole)
 
 
