@@ -25,6 +25,7 @@ template <int D, bool BF16> struct PromptSizes {
   static constexpr int UNIT = RECS * kKvGroup;
   static_assert(UNIT == kv_prompt_unit(D), "the host shares out the kernel's units");
   static constexpr int NQ = BF16 ? 1 : 3, NP = BF16 ? 1 : 2;
+  static constexpr int SIDE = QT == 1 && RECS == 4 ? 4 : 2;  // records, with QT four sums, whose products alternate
   static constexpr int KOPS = RECS * (D / 32), VOPS = RECS / 2 * (D / 16);  // operands of a step, 1 KB each
   static constexpr int PART = R * (D + 2);
 };
@@ -264,17 +265,16 @@ template <int D, bool BF16> __global__ __launch_bounds__(kKvThreads, 2) void k_k
 #pragma unroll
           for (int s = 0; s < Z::RECS; ++s) z[t][s] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int s0 = 0; s0 < Z::RECS; s0 += 2)
+        for (int s0 = 0; s0 < Z::RECS; s0 += Z::SIDE)
 #pragma unroll
           for (int j = 0; j < D / 32; ++j)
 #pragma unroll
-            for (int s = s0; s < s0 + 2; ++s) {
-              const bf16x8 k = ko[(s * (D / 32) + j) * 64];
+            for (int n = Z::NQ - 1; n >= 0; --n)
 #pragma unroll
-              for (int n = Z::NQ - 1; n >= 0; --n)
+              for (int s = s0; s < s0 + Z::SIDE; ++s)
 #pragma unroll
-                for (int t = 0; t < QT; ++t) z[t][s] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, q[t][n][j], z[t][s], 0, 0, 0);
-            }
+                for (int t = 0; t < QT; ++t)  // (a sum's next product waits for its last)
+                  z[t][s] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ko[(s * (D / 32) + j) * 64], q[t][n][j], z[t][s], 0, 0, 0);
         __builtin_amdgcn_s_setprio(1);  // (the other wave's products need no issue while they run)
         uint32_t odd = 0;
 #pragma unroll
@@ -285,13 +285,14 @@ template <int D, bool BF16> __global__ __launch_bounds__(kKvThreads, 2) void k_k
           f16x8 part[QT][Z::NP];
           weight_operands<QT, Z::NP, Z::RECS>(z, s0, part);
 #pragma unroll
-          for (int j = 0; j < D / 16; ++j) {
-            const f16x8 v = vo[(s0 / 2 * (D / 16) + j) * 64];
+          for (int j0 = 0; j0 < D / 16; j0 += 4 / QT)
 #pragma unroll
             for (int n = Z::NP - 1; n >= 0; --n)
 #pragma unroll
-              for (int t = 0; t < QT; ++t) w.o[t][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, part[t][n], w.o[t][j], 0, 0, 0);
-          }
+              for (int j = j0; j < j0 + 4 / QT; ++j)
+#pragma unroll
+                for (int t = 0; t < QT; ++t)
+                  w.o[t][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vo[(s0 / 2 * (D / 16) + j) * 64], part[t][n], w.o[t][j], 0, 0, 0);
         }
         __builtin_amdgcn_s_setprio(0);
         if (__builtin_expect(uniform_u32(odd) != 0, 0)) {
