@@ -162,7 +162,7 @@ Shape shape_of(int N, int B, int hq, int hkv, int d, bool bf16, bool planned) {
   s.R = s.prompt ? kv_prompt_rows(d, bf16) : 16 * s.qt;
   s.unit = s.prompt ? kv_prompt_unit(d) : kKvRowsUnit;
   s.lead = s.prompt ? kKvPromptLead : kKvRowsLead;
-  s.blocks = s.prompt ? prompt_blocks(d) : 256 * kv_rows_waves(d, s.qt);
+  s.blocks = s.prompt ? prompt_blocks(d) : 256 * kv_rows_waves(d, s.qt, bf16);
   s.tiles = planned ? (size_t)(((long long)N * G + s.R - 1) / s.R + B) : (size_t)B * ((G + s.R - 1) / s.R);
   const size_t listed = planned ? s.tiles : 0;
   s.off_plan = 256;
@@ -208,7 +208,7 @@ size_t kv_attention_bytes(int N, int B, int hq, int hkv, int d, bool bf16, bool 
 size_t kv_attention_most(int N, int B, int hq, int hkv, int d) {
   const size_t tiles = ((size_t)N * (hq / hkv) + 15) / 16 + B;
   size_t part = 0;
-  for (int qt = 1; qt <= 2; ++qt) part = std::max(part, part_bytes(d, 16 * qt, 256 * kv_rows_waves(d, qt)));
+  for (int qt = 1; qt <= 2; ++qt) part = std::max(part, part_bytes(d, 16 * qt, 256 * kv_rows_waves(d, qt, true)));
   part = std::max(part, part_bytes(d, kv_prompt_rows(d, true), prompt_blocks(d)));
   return 256 + up256(tiles * sizeof(KvPlanEntry)) + up256(tiles * 4) + up256((size_t)(B + 1) * 4) + up256(kMostBlocks * 40) + part;
 }

@@ -708,9 +708,10 @@ __device__ __forceinline__ void products(KvSums<D, QT>& w, const uint32_t (&v)[2
 
 // ---- kernels ----------------------------------------------------------------------------------
 
-// Waves of a SIMD of the rows' kernel, which is blocks of a compute unit: what the registers
-// of its loop allow.
-constexpr int kv_rows_waves(int d, int qt) { return d * qt == 64 ? 3 : 2; }
+// Waves of a SIMD of the rows' kernel, which is blocks of a compute unit: what its registers
+// allow.  (A kernel that spills any takes 6 us longer to start: with two waves the widest fp32 rows
+// take 14.4 us instead of 8.8 for 200 tiles of 4 tokens, 49 instead of 28.5 behind 16 times 8192.)
+constexpr int kv_rows_waves(int d, int qt, bool bf16) { return d * qt == 64 ? 3 : d * qt == 256 && !bf16 ? 1 : 2; }
 // Tokens of a unit, and the units that a tile costs besides its own.
 constexpr int kKvRowsUnit = 128, kKvRowsLead = 3, kKvPromptLead = 3;
 constexpr int kv_prompt_unit(int d) { return d == 256 ? 32 : 64; }

@@ -40,7 +40,7 @@ template <int D, int QT, bool BF16> struct Sizes {
   static constexpr int PITCH = D + 4;
   static constexpr int SOBYTES = kWaves * 16 * PITCH * 4;
   static constexpr int POOL = QBYTES > SOBYTES ? QBYTES : SOBYTES;
-  static constexpr int WAVES = kv_rows_waves(D, QT);
+  static constexpr int WAVES = kv_rows_waves(D, QT, BF16);
   static constexpr int DEPTH = 2;  // steps whose loads are under way
   static constexpr int PART = R * (D + 2);  // floats of a partial sum: o, then m, then l
 };
