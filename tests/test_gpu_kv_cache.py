@@ -134,6 +134,8 @@ def test_more_threads_than_a_launch_holds():
     rk, rv = P.kv_read(cache, slots.cuda(), dtype=BF16)
     for r in (rk, rv):
         assert torch.equal(r[some.cuda()].cpu().double(), held(k))
+    del rk, rv, r
+    torch.cuda.empty_cache()  # (70 GB)
 
 
 def test_graph_and_streams():
