@@ -15,6 +15,16 @@ constexpr float kLow = -3.402823466e+38f;  // maximum of a row that has seen no 
 constexpr float kLead = 7.f, kLazy = 8.f;
 // Up to here a maximum is off by half at most: the exponents, which are exact, stay below 16.
 constexpr float kFar = 8388608.f;
+// A cached value is below 2^127.6 (6 * 2^125), a weight 2^15 at most, a sequence has 2^30 tokens at
+// most: with scales below 2^65 O stays below 2^(67.6 + 15 + 30), whatever is joined.  Where there are larger
+// ones O is looked at behind a wave's last step.  If some rows left fp32, the wave's are done once more,
+// these and those of kTall and more with weights 2^-kLift of what they were (O is below 2^(127.6 +
+// 15 + 30 - 48) then), which loses what is below 2^-84 of each token's: fp32's least normal number by a
+// largest weight of 2^(7 - 48).  Else O of kTall or more is made 2^-kLower as large, so that the
+// sum of a row's parts (four waves of 768 blocks at most) stays in range.
+constexpr uint32_t kHighScale = 192;  // 2^65: a byte's upper two bits
+constexpr int kLift = 48, kLower = 16;
+constexpr uint32_t kTall = (127u + 112u) << 23;  // 2^112
 
 // ---- the work of a call -------------------------------------------------------------
 
@@ -524,7 +534,20 @@ template <int D, int QT> struct KvSums {
   int pos[QT];          // the row's position, -1 and less: sees nothing
   bool far;             // some row's m is beyond kFar; then c is 1 and off 0, else a.c and m
   float c, off[QT];
+  bool large;           // there were value scales of kHighScale and more
 };
+
+template <int D, int QT> __device__ __forceinline__ void clear(KvSums<D, QT>& w, const KvAttentionArgs& a) {
+  w.far = w.large = false;
+  w.c = a.c;
+#pragma unroll
+  for (int t = 0; t < QT; ++t) {
+    w.m[t] = w.off[t] = kLow;
+    w.l[t] = 0.f;
+#pragma unroll
+    for (int j = 0; j < D / 16; ++j) w.o[t][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+}
 
 // The softmax of a step: scores z of the tokens of U records from tok on become weights, the
 // sums what they are counted from.  `masked`: not every row sees all of the tokens.
@@ -639,12 +662,15 @@ __device__ __forceinline__ void wide_products(KvSums<D, QT>& w, const uint32_t (
 // is not: scales of NaN (and the two whose values leave fp32, which are in a cache only
 // where nothing was written) become 1, and the rows that see such a token NaN in its columns.
 // The product of f16 operands follows in every step, here with values of 0 (no_values): where
-// it followed in other steps alone, every step copied the sums.
+// it followed in other steps alone, every step copied the sums.  lost: bit t: the lane's row has
+// weights 2^-kLift as large.
 template <int D, int QT, int U>
 __device__ __forceinline__ void wide_values(KvSums<D, QT>& w, const KvAttentionArgs& a, const uint32_t (&v)[2][D / 32],
-                                            const uint32_t (&scales)[2], const f32x4 (&p)[QT][U], int first, int tok) {
+                                            const uint32_t (&scales)[2], const f32x4 (&p)[QT][U], int first, int tok,
+                                            uint32_t lost = 0) {
   const int lane = threadIdx.x % 64, g = lane / 16;
   uint32_t odd = 0, vs[2] = {scales[0], scales[1]};
+  if (__ballot((((vs[0] & vs[0] << 1) | (vs[1] & vs[1] << 1)) & 0x80808080u) != 0)) w.large = true;
   float sc[2][4];
 #pragma unroll
   for (int u = 0; u < 2; ++u)
@@ -676,7 +702,8 @@ __device__ __forceinline__ void wide_values(KvSums<D, QT>& w, const KvAttentionA
   bf16x8 part[QT][3];
 #pragma unroll
   for (int t = 0; t < QT; ++t) {
-    const f32x4 x = p[t][first], y = p[t][first + 1];
+    const float as = lost >> t & 1u ? 0x1p-48f : 1.f;
+    const f32x4 x = p[t][first] * as, y = p[t][first + 1] * as;
     const float e[8] = {x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
     split8(e, part[t]);
   }
@@ -704,6 +731,95 @@ __device__ __forceinline__ void products(KvSums<D, QT>& w, const uint32_t (&v)[2
       for (int j = 0; j < 2; ++j)
         w.o[t][2 * C + j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f[j], part[t][n], w.o[t][2 * C + j], 0, 0, 0);
   if constexpr (C + 1 < D / 32) products<D, C + 1, QT, NP>(w, v, sc, part);
+}
+
+// ---- large values -----------------------------------------------------------------------------
+
+// The largest magnitude of a row's O, as bits (an infinity, or above it NaN); 0 for a row that is NaN by
+// its scores.
+template <int D, int QT> __device__ __forceinline__ uint32_t tallest(const KvSums<D, QT>& w, int t) {
+  uint32_t top = w.l[t] != w.l[t] ? ~0u : 0u;
+#pragma unroll
+  for (int j = 0; j < D / 16; ++j)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) top = max(top, __float_as_uint(w.o[t][j][i]) & 0x7fffffffu);
+  top = max(top, (uint32_t)__shfl_xor((int)top, 16));
+  top = max(top, (uint32_t)__shfl_xor((int)top, 32));
+  return top == ~0u ? 0u : top;
+}
+
+// Makes m of a row whose O is smaller (lost), or is to be, what O is counted from; l follows, so that
+// whoever joins sums need not know.  m is rounded up in front of the addition, which is exact then,
+// and what that moves it by goes into l and O alike.  (Beyond 2^28 the sum may not be a float: O is
+// as it would be without; weights are 0 or equal there, and only sums of equal ones can pass fp32.)
+template <int D, int QT> __device__ __forceinline__ void settle(KvSums<D, QT>& w, uint32_t lost) {
+  static_assert(kLift == 48, "the power below, and wide_values'");
+#pragma unroll
+  for (int t = 0; t < QT; ++t) {
+    const bool small = lost >> t & 1u;
+    const uint32_t top = tallest<D, QT>(w, t);
+    const float add = small ? (float)kLift : top >= kTall && top < 0x7f800000u ? (float)kLower : 0.f;
+    const float to = ceilf(w.m[t]) + add, by = w.m[t] - to;
+    const bool can = add > 0.f && by <= -add && by > -(add + 1.f);
+    const float f = can ? __builtin_amdgcn_exp2f(by) : 1.f;
+    w.m[t] = can ? to : w.m[t];
+    w.l[t] *= f;
+#pragma unroll
+    for (int j = 0; j < D / 16; ++j) w.o[t][j] *= small ? f * 0x1p48f : f;
+  }
+}
+
+// Behind a wave's steps, where there were large values (w.large).  The second time a wave is by itself: it
+// reads the records for tokens tok, tok + stride .. below end, 32 at a time, and has wide_values do all
+// values; q(t, n, j) is an operand of its rows.  Calls without large values take 0 to 2% longer for the code
+// that is jumped over; 16 tokens behind 2048, all values near 2^124, 32 us instead of 17, a prompt of
+// 2048 rows 239 instead of 71.
+template <int D, int QT, int NQ, typename Q>
+__device__ __forceinline__ void large_values(KvSums<D, QT>& w, const KvAttentionArgs& a, const KvRecords<D>& records, int tok, int end,
+                                             int stride, int hi, const Q& q) {
+  asm volatile("");
+  uint32_t lost = 0;  // (what a row's weights are counted from may differ by 2^8 the second time: tall ones too)
+  bool any = false;
+#pragma unroll
+  for (int t = 0; t < QT; ++t) {
+    const uint32_t top = tallest<D, QT>(w, t);
+    lost |= top >= kTall ? 1u << t : 0u;
+    any |= top >= 0x7f800000u;
+  }
+  if (__ballot(any) == 0) lost = 0;
+  if (__ballot(any)) {
+    const int g = threadIdx.x % 64 / 16;
+    const KvLane<D> off;
+    clear(w, a);
+#pragma unroll 1
+    for (; tok < end; tok += stride) {
+      f32x4 z[QT][2];
+      uint32_t v[2][D / 32], vs[2];
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const typename KvRecords<D>::Place at = records.find((uint32_t)tok / kKvGroup + u);
+        const __amdgpu_buffer_rsrc_t r = records.at(at);
+        uint32_t k[D / 32];
+        load_words<D / 32, false>(r, off.k, k);
+        load_words<D / 32, false>(r, off.v, v[u]);
+        const uint32_t ks = load_key_scales<D>(r, off.ks) | records.bad(at);
+        vs[u] = hidden_as_one(__builtin_amdgcn_raw_buffer_load_b32(r, (int)off.vs, 0, 0), tok + 16 * u + 4 * g, hi);
+#pragma unroll
+        for (int t = 0; t < QT; ++t) z[t][u] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int n = NQ - 1; n >= 0; --n)
+#pragma unroll
+          for (int j = 0; j < D / 32; ++j) {
+            const bf16x8 key = eight_of(k[j], D == 256 && j >= 4 ? kv_scale(ks >> 8 & 0xffu) : kv_scale(ks & 0xffu));
+#pragma unroll
+            for (int t = 0; t < QT; ++t) z[t][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(key, q(t, n, j), z[t][u], 0, 0, 0);
+          }
+      }
+      weights<D, QT, 2>(w, a, z, tok, true);
+      wide_values<D, QT, 2>(w, a, v, vs, z, 0, tok, lost);
+    }
+  }
+  settle<D, QT>(w, lost);
 }
 
 // ---- kernels ----------------------------------------------------------------------------------

@@ -177,8 +177,7 @@ template <int D, bool BF16> __global__ __launch_bounds__(kKvThreads, 2) void k_k
 
     // the wave's rows
     KvSums<D, QT> w;
-    w.far = false;
-    w.c = a.c;
+    clear<D, QT>(w, a);
     bf16x8 q[QT][Z::NQ][D / 32];
     const int mine = wave * 16 * QT;
 #pragma unroll
@@ -186,8 +185,6 @@ template <int D, bool BF16> __global__ __launch_bounds__(kKvThreads, 2) void k_k
       const int r = min(mine + t * 16 + lane % 16, tile.rows - 1);  // (rows behind the last repeat it and are not stored)
       const int i = (tile.row0 + r) / G, head = h * G + (tile.row0 + r) % G;
       w.pos[t] = tile.len - tile.nq + i;
-      w.m[t] = w.off[t] = kLow;
-      w.l[t] = 0.f;
       const size_t at = ((size_t)(tile.start + i) * a.hq + head) * D + g * (D / 4);
 #pragma unroll
       for (int j = 0; j < D / 32; ++j) {
@@ -196,8 +193,6 @@ template <int D, bool BF16> __global__ __launch_bounds__(kKvThreads, 2) void k_k
 #pragma unroll
         for (int n = 0; n < Z::NQ; ++n) q[t][n][j] = part[n];
       }
-#pragma unroll
-      for (int j = 0; j < D / 16; ++j) w.o[t][j] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
     // positions of its first and last row; none: a last one that sees nothing
     const int base = tile.len - tile.nq;
@@ -313,6 +308,18 @@ template <int D, bool BF16> __global__ __launch_bounds__(kKvThreads, 2) void k_k
       }
       lds_barrier();
     }
+    if (__builtin_expect(w.large, 0))
+      large_values<D, QT, Z::NQ>(w, a, records, tile.lo + p.u0 * Z::UNIT, min(tile.hi, tile.lo + p.u1 * Z::UNIT), 2 * kKvGroup, tile.hi,
+                                 [&](int t, int n, int j) {
+                                   if constexpr (Z::NQ * D <= 512) return q[t][n][j];
+                                   // (no registers for them there)
+                                   int r = mine + t * 16 + lane % 16;
+                                   asm volatile("" : "+v"(r));
+                                   const int row = tile.row0 + min(r, tile.rows - 1);
+                                   bf16x8 part[Z::NQ];
+                                   load_q8<Z::NQ>(a.q, ((size_t)(tile.start + row / G) * a.hq + h * G + row % G) * D + g * (D / 4) + 8 * j, part);
+                                   return part[n];
+                                 });
 
 #pragma unroll
     for (int t = 0; t < QT; ++t) {

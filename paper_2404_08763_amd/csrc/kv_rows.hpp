@@ -55,15 +55,12 @@ template <int D, int QT, bool BF16>
 __device__ __forceinline__ void load_q(Wave<D, QT, BF16>& w, const KvAttentionArgs& a, int h, const KvTile& tile, bf16x8* sq) {
   typedef Sizes<D, QT, BF16> Z;
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, g = lane / 16, G = a.hq / a.hkv;
-  w.far = false;
-  w.c = a.c;
+  clear<D, QT>(w, a);
 #pragma unroll
   for (int t = 0; t < QT; ++t) {
     const int r = min(t * 16 + lane % 16, tile.rows - 1);  // (rows behind the last repeat it and are not stored)
     const int i = (tile.row0 + r) / G, head = h * G + (tile.row0 + r) % G;
     w.pos[t] = tile.len - tile.nq + i;
-    w.m[t] = w.off[t] = kLow;
-    w.l[t] = 0.f;
     const size_t at = ((size_t)(tile.start + i) * a.hq + head) * D + g * (D / 4);
     if constexpr (Z::QLDS) {
 #pragma unroll
@@ -83,8 +80,6 @@ __device__ __forceinline__ void load_q(Wave<D, QT, BF16>& w, const KvAttentionAr
         for (int n = 0; n < Z::NQ; ++n) w.q[t][n][j] = part[n];
       }
     }
-#pragma unroll
-    for (int j = 0; j < D / 16; ++j) w.o[t][j] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
   if constexpr (Z::QLDS) __syncthreads();
 }
@@ -301,6 +296,12 @@ __global__ __launch_bounds__(kThreads, (Sizes<D, QT, BF16>::WAVES)) void k_kv_ro
         }
       } while (tok < end);
     }
+
+    if (__builtin_expect(uniform_u32(w.large ? 1 : 0) != 0, 0))
+      large_values<D, QT, Z::NQ>(w, a, records, tile.lo + p.u0 * kUnit + wave * kStep, end, kUnit, tile.hi, [&](int t, int n, int j) {
+        if constexpr (Z::QLDS) return sq[((t * Z::NQ + n) * (D / 32) + j) * 64 + lane];
+        else return w.q[t][n][j];
+      });
 
     // the waves' sums together, 16 rows at a time
 #pragma unroll
