@@ -760,7 +760,7 @@ template <int D, int QT> __device__ __forceinline__ void settle(KvSums<D, QT>& w
     const uint32_t top = tallest<D, QT>(w, t);
     const float add = small ? (float)kLift : top >= kTall && top < 0x7f800000u ? (float)kLower : 0.f;
     const float to = ceilf(w.m[t]) + add, by = w.m[t] - to;
-    const bool can = add > 0.f && by <= -add && by > -(add + 1.f);
+    const bool can = add > 0.f && by <= -add && by >= -(add + 1.f);  // (m next to the integer below rounds to the latter)
     const float f = can ? __builtin_amdgcn_exp2f(by) : 1.f;
     w.m[t] = can ? to : w.m[t];
     w.l[t] *= f;

@@ -124,3 +124,34 @@ def test_weights_at_their_largest(rows, power, dtype):
     want, bound = attention(q[pick].to(dtype), ks, vs, [n, n], None if rows == 1 else [0, rows, 2 * rows], 0, scale)
     near(got[pick.cuda()], want, bound)
     assert torch.isfinite(got).all()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=IDS.get)
+@pytest.mark.parametrize("counts", [None, [2, 2, 2, 2, 90]], ids=["rows", "ragged"])
+@pytest.mark.parametrize("power", [100, 123])
+def test_maxima_next_to_integers(power, counts, dtype):
+    """Maxima of a few steps of fp32 above and below integers (in base 2): one key column, equal scores."""
+    say("kv maxima next to integers", power, counts, dtype)
+    lens = [40, 100, 130, 2, 150]
+    b = Batch(lens, 4, 2, 64, 16, dtype, counts=counts, seed=95, far=(float(power),))
+    for s, n in enumerate(lens):
+        k = torch.zeros(n, 2, 64)
+        k[..., 0] = 1.0
+        t = torch.arange(n)
+        pages = torch.tensor(b.pages[s])
+        cache = b.cache.cuda()
+        slots = (pages[t // 16] * 16 + t % 16).to(torch.int32).cuda()
+        _, v = P.kv_read(cache, slots, dtype=F32)
+        P.kv_write(cache, k.cuda(), v, slots)
+        b.cache = cache.cpu()
+        b.k[s] = k.double()
+    g = gen(96)
+    whole = torch.randint(-9, 9, b.q.shape[:2], generator=g).float()
+    steps = torch.randint(-3, 4, b.q.shape[:2], generator=g).float()
+    b.q.zero_()
+    b.q[..., 0] = (whole * (1 + steps * 2.0 ** -23)).to(dtype)
+    scale = 0.6931471805599453  # its product with log2(e) is 1, or a step of fp32 beside it
+    q, cache, table, ln, start = b.device()
+    got = P.kv_attention(q, cache, table, ln, q_start=start, scale=scale)
+    want, bound = b.expect(0, scale)
+    near(got, want, bound + lost(b, 0))
