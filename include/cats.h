@@ -446,7 +446,8 @@ cats_status cats_linear_fp8(const void* xq, const void* xs, int32_t N, const voi
  *   (u, w) -> (u cos a - w sin a, w cos a + u sin a); columns from rot on stay.
  *   gain_q, gain_k  dev [d] fp32, or NULL: 1 (read with norm only)
  *   pos, freq       dev [N] int32, dev [rot/2] fp32 (not read if rot is 0); the
- *                   product is taken in 64 bits, so positions far out lose nothing
+ *                   angle is held in 64 bits (off by 3 * 2^-53 of itself), its
+ *                   sine and cosine are fp32's, also next to 0
  *   q, k            dev [N x hq x d], [N x hkv x d], odtype fp32 or bf16, rounded
  *                   once; must not overlap the inputs
  * A head whose squares leave fp32's range becomes 0 (as cats_rmsnorm's rows).
