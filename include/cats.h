@@ -518,7 +518,8 @@ cats_status cats_kv_read(const cats_kv_cache* cache, const int32_t* slots, int32
  * on the other sequences of the call (how the keys are shared out), but not from
  * run to run.
  * Workspace: cats_kv_attention_workspace_bytes(N, B, hq, heads, d), which serves
- * every call of up to as many rows and sequences of the same heads.
+ * every call of up to as many rows and sequences of the same heads: 64 MiB at most,
+ * and 12 bytes for each 16 rows of a key head, 16 for each sequence.
  * 1 <= N, B <= CATS_MAX_KV_ROWS, hq a multiple of heads, scale > 0, window >= 0.
  * CATS_ERR_SHAPE also where the tiles of 16 to 128 rows times the units of 32 to
  * 128 tokens of a table's row reach 2^31: a prompt of 2^20 rows and one query head for

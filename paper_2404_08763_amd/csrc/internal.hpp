@@ -330,9 +330,10 @@ struct KvAttentionArgs {
   KvPlanEntry* plan;     // null: each block makes its own
   int* prefix;           // what is in front of each tile (KvRun)
   int* first;            // [B + 1] first tile of each sequence
-  int parts;             // without a plan: parts of a tile that tickets join (64 KB); 0: a last kernel does
+  int parts;             // not 0: tickets join a tile's parts (single rows: this many at about 64 KB; prompts:
+                         // 1, any number); 0: a last kernel does
   uint32_t epoch;        // the tickets' tag
-  unsigned long long* tickets;  // [blocks] of the sum that begins in each block
+  unsigned long long* tickets;  // [blocks] of the sum that begins in each block; prompts: [5][blocks]
   // for the last kernel: {parts | first block << 16, h, b, row0} of a tile, in order of the tiles
   // where there are fewer than blocks (by_tile), else of the block that it begins in
   int4* desc;            // [sums]

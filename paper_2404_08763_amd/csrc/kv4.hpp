@@ -18,13 +18,11 @@
 namespace cats {
 
 constexpr int kKvGroup = 16;  // tokens of a record
-constexpr int kKvBlock = 32;  // columns that share a scale
 constexpr int kKvMinExp = -125, kKvMaxExp = 125;
 
 __host__ __device__ constexpr int kv_record_bytes(int d) { return 17 * d; }
 
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 

@@ -148,8 +148,14 @@ constexpr size_t up256(size_t v) { return (v + 255) / 256 * 256; }
 constexpr int kMostBlocks = 768;
 size_t part_bytes(int d, int R, int blocks) { return (size_t)blocks * 2 * R * (d + 2) * 4; }
 
-// Two to a compute unit; fewer where their partial sums would take more than 61 MiB.
-int prompt_blocks(int d) { return d == 64 ? 512 : 480; }
+// Two to a compute unit; fewer where a workspace without its lists would pass 64 MiB: 496 for bf16 rows of
+// 128 columns, 504 for 256 columns.  (A bf16 prompt of 4096 rows takes 172 us with 512, 178 with 496, 183 with
+// 480; one of fp32 rows 292 with 512, 308 with 480.)
+constexpr size_t kMostWorkspace = (size_t)64 << 20;
+int prompt_blocks(int d, bool bf16) {
+  const size_t fit = (kMostWorkspace - 256 - up256(kMostBlocks * 40)) / part_bytes(d, kv_prompt_rows(d, bf16), 1);
+  return (int)std::min<size_t>(512, fit / 8 * 8);
+}
 
 Shape shape_of(int N, int B, int hq, int hkv, int d, bool bf16, bool planned) {
   Shape s{};
@@ -162,7 +168,7 @@ Shape shape_of(int N, int B, int hq, int hkv, int d, bool bf16, bool planned) {
   s.R = s.prompt ? kv_prompt_rows(d, bf16) : 16 * s.qt;
   s.unit = s.prompt ? kv_prompt_unit(d) : kKvRowsUnit;
   s.lead = s.prompt ? kKvPromptLead : kKvRowsLead;
-  s.blocks = s.prompt ? prompt_blocks(d) : 256 * kv_rows_waves(d, s.qt, bf16);
+  s.blocks = s.prompt ? prompt_blocks(d, bf16) : 256 * kv_rows_waves(d, s.qt, bf16);
   s.tiles = planned ? (size_t)(((long long)N * G + s.R - 1) / s.R + B) : (size_t)B * ((G + s.R - 1) / s.R);
   const size_t listed = planned ? s.tiles : 0;
   s.off_plan = 256;
@@ -209,7 +215,7 @@ size_t kv_attention_most(int N, int B, int hq, int hkv, int d) {
   const size_t tiles = ((size_t)N * (hq / hkv) + 15) / 16 + B;
   size_t part = 0;
   for (int qt = 1; qt <= 2; ++qt) part = std::max(part, part_bytes(d, 16 * qt, 256 * kv_rows_waves(d, qt, true)));
-  part = std::max(part, part_bytes(d, kv_prompt_rows(d, true), prompt_blocks(d)));
+  for (const bool bf16 : {false, true}) part = std::max(part, part_bytes(d, kv_prompt_rows(d, bf16), prompt_blocks(d, bf16)));
   return 256 + up256(tiles * sizeof(KvPlanEntry)) + up256(tiles * 4) + up256((size_t)(B + 1) * 4) + up256(kMostBlocks * 40) + part;
 }
 
@@ -234,8 +240,9 @@ hipError_t launch_kv_attention(KvAttentionArgs a, int d, bool bf16, hipStream_t 
   const long long split_in = std::min<long long>(units_most(a, sh.unit), sh.blocks / ((long long)sh.tiles * a.hkv) + 2);
   a.parts = !a.q_start && split_in * row_bytes <= (64 << 10) ? (64 << 10) / row_bytes : 0;
   // So do the blocks of a prompt with a tile for every other block or more, whose tiles are in
-  // three parts or less (1024 tiles for 480 blocks 186 us instead of 195, 256 tiles 37 instead of
-  // 44; 188 tiles 49 instead of 45, 128 tiles 33 instead of 32).
+  // three parts or less where they are alike, in tens where one is far longer (1024 tiles for 480
+  // blocks 186 us instead of 195, 256 tiles 37 instead of 44; 188 tiles 49 instead of 45, 128 tiles 33
+  // instead of 32).
   if (sh.prompt && (long long)a.N * (a.hq / a.hkv) / sh.R * a.hkv >= sh.blocks / 2) a.parts = 1;
   a.tickets = reinterpret_cast<unsigned long long*>(a.desc);
   a.epoch = call_epoch();

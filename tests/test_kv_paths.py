@@ -4,6 +4,8 @@ import math
 import pytest
 import torch
 
+import paper_2404_08763_amd as P
+
 import kv_paths
 from kv_util import BF16, F32, attention, gen
 
@@ -25,3 +27,12 @@ def test_same_as_the_definition(counts, window, dtype):
     assert torch.allclose(got, want, rtol=1e-12, atol=1e-14, equal_nan=True)
     fine = ~torch.isnan(want)
     assert torch.allclose(other[fine], bound[fine], rtol=1e-9, atol=1e-20)
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("hq,hkv", [(1, 1), (32, 8), (40, 1), (1024, 1)])
+def test_workspace_as_stated(hq, hkv, d):
+    """64 MiB, and 12 bytes for each 16 rows of a key head and 16 for each sequence."""
+    f = P.raw().cats_kv_attention_workspace_bytes
+    for N, B in ((1, 1), (4096, 1), (4096, 64), (700, 700), (1 << 20, 1), (1 << 20, 1 << 20)):
+        assert 0 < f(N, B, hq, hkv, d) <= (64 << 20) + 12 * -(-N * (hq // hkv) // 16) + 16 * B
