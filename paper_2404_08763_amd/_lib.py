@@ -816,9 +816,9 @@ def qk_norm_rope(qkv: torch.Tensor, heads: int, kv_heads: int, d: int, pos: Opti
     if freq is not None:
         if pos is None:
             raise ValueError("freq needs pos")
-        half = freq.shape[0]
         if freq.dim() != 1:
             raise ValueError(f"freq must have one dimension, got shape {list(freq.shape)}")
+        half = freq.shape[0]
         if pos.shape != (N,):
             _shape_is(pos, (N,), "pos")
         if freq.dtype is not torch.float32 or freq.get_device() != device or not freq.is_contiguous():
