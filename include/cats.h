@@ -450,7 +450,8 @@ cats_status cats_linear_fp8(const void* xq, const void* xs, int32_t N, const voi
  *                   sine and cosine are fp32's, also next to 0
  *   q, k            dev [N x hq x d], [N x hkv x d], odtype fp32 or bf16, rounded
  *                   once; must not overlap the inputs
- * A head whose squares leave fp32's range becomes 0 (as cats_rmsnorm's rows).
+ * A head whose squares pass fp32's range becomes 0 (as cats_rmsnorm's rows); small ones
+ * keep their digits whatever eps is (zeros with eps = 0 are NaN).
  * 1 <= N <= CATS_MAX_KV_ROWS, d a multiple of 8 up to 512, rot a multiple of 8
  * up to d; all but pos 16-byte aligned. */
 cats_status cats_qk_norm_rope(const void* qkv, int32_t dtype, int64_t ld, int32_t N, int32_t hq, int32_t hkv, int32_t d,

@@ -21,6 +21,7 @@ namespace cats {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr float kTiny = 0x1p-100f;
 
 // Four elements as they are in memory.
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
@@ -117,7 +118,21 @@ template <int L, bool XB, bool YB> __global__ __launch_bounds__(kThreads) void k
 #pragma unroll
       for (int i = 0; i < 4; ++i) q = fmaf(u[i], u[i], fmaf(w[i], w[i], q));
       q = lanes_sum<L>(q);
-      const float r = 1.f / sqrtf(q / (float)a.d + a.eps);
+      float eps = a.eps;
+      if (a.eps < kTiny) {
+        // squares below 2^-100 in all lose digits, which only so small an eps shows: those of 2^100 x
+        const float up = q < kTiny ? 0x1p100f : 1.f;
+        q = 0.f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          u[i] *= up;
+          w[i] *= up;
+          q = fmaf(u[i], u[i], fmaf(w[i], w[i], q));
+        }
+        q = lanes_sum<L>(q);
+        eps = eps * up * up;
+      }
+      const float r = 1.f / sqrtf(q / (float)a.d + eps);
       const float* gain = h < a.hq ? a.gq : a.gk;
       if (gain && on) {
         const f32x4 ga = *reinterpret_cast<const f32x4*>(gain + ca), gb = *reinterpret_cast<const f32x4*>(gain + cb);
