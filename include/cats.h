@@ -515,9 +515,16 @@ cats_status cats_kv_read(const cats_kv_cache* cache, const int32_t* slots, int32
  * Masked tokens have no effect, whatever the cache holds for them.
  * Products of q and the cache's values are exact and summed in fp32, as is the
  * softmax; its weights enter the second product rounded to f16 (11 bits) for
- * bf16 rows, as two such parts (22 bits) for fp32 rows.  A row's bits may depend
- * on the other sequences of the call (how the keys are shared out), but not from
- * run to run.
+ * bf16 rows, as two such parts (22 bits) for fp32 rows, but no finer than 2^-32 of
+ * the row's largest weight for each token (65536 small equal weights beside a large
+ * one: 2^-16 of their values at most).  Values may be as
+ * large as the cache holds them: sums that would leave fp32 are scaled, which loses
+ * what is below 2^-84 for each token.  A row's bits may depend
+ * on the other sequences of the call (how the keys are shared out) and, where values pass
+ * 2^64, on the rows beside it, but not from run to run.
+ * The kernel is chosen by the rows that a sequence has on average: a few single
+ * tokens beside a prompt cost little, but many of them with a chunk take up to 2.4
+ * times as long in one call as in two, the single tokens without q_start.
  * Workspace: cats_kv_attention_workspace_bytes(N, B, hq, heads, d), which serves
  * every call of up to as many rows and sequences of the same heads: 64 MiB at most,
  * and 12 bytes for each 16 rows of a key head, 16 for each sequence.

@@ -14,7 +14,9 @@
 // The scores, P before its rounding, the statistics and O are fp32.  The second product
 // is one of f16, which has the cache's values exactly (but for scales far out, see
 // wide_values) and P with 11 bits for bf16 rows, an eighth of their own rounding, and in
-// two parts with 22 for fp32 rows, whose q is split in three bf16 parts, all 24 bits.
+// two parts with 22 for fp32 rows, whose q is split in three bf16 parts, all 24 bits.  P's
+// steps end at f16's least, 2^-24 of weights that are 2^7 or more where they are largest: its
+// error is 2^-32 of a row's largest weight for each token where that is more.
 //
 // One kernel takes few rows of each sequence (kv_rows.hpp), another many (kv_prompt.hpp).
 // The blocks share all of a call's keys evenly, whatever the sequences' lengths (KvRun): what

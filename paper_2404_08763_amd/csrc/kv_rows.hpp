@@ -5,9 +5,10 @@
 // registers: no step waits for another wave.  Two steps' loads are under way; a block's
 // four waves take every fourth step of its tokens and add their sums through LDS.
 // 8 key heads of 128 columns with 4 query heads each, 32 sequences (311 MB of cache in all):
-// 57 us, 5.5 TB/s; 32 heads of their own, 16 sequences (95 MB): 26.5 us, of which the bytes
-// would be 13 at a plain read's rate, and the launch, the first tile's place, its first loads and
-// the last sums are the rest.
+// 57.5 us, 5.4 TB/s; 32 heads of their own, 16 sequences (95 MB): 27.2 us, of which the bytes
+// would be 13 at a plain read's rate.  The rest is the launch, and what a tile's end and the next one's start
+// leave empty: no key is under way while the sums are joined and the next tile's length, table and q
+// are read, and a tile's last two steps load its last record again for nothing.
 #pragma once
 
 #include "kv_attention.hpp"
