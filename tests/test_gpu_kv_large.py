@@ -13,6 +13,7 @@ import torch
 
 import paper_2404_08763_amd as P
 
+import kv_paths
 from gpu_util import say
 from kv_util import BF16, F32, Batch, attention, gen, held
 
@@ -155,3 +156,37 @@ def test_maxima_next_to_integers(power, counts, dtype):
     got = P.kv_attention(q, cache, table, ln, q_start=start, scale=scale)
     want, bound = b.expect(0, scale)
     near(got, want, bound + lost(b, 0))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=IDS.get)
+@pytest.mark.parametrize("hq,hkv,d", [(4, 1, 64), (20, 1, 64), (8, 2, 128), (4, 2, 256), (32, 1, 128)])
+@pytest.mark.parametrize("far", [(100.0,), (124.0,), (124.0, 0.0)])
+@pytest.mark.parametrize("rows", [None, [1, 4, 2]], ids=["rows", "ragged"])
+def test_long_sequences_of_large_values(rows, far, hq, hkv, d, dtype):
+    """Single tokens and few rows whose keys are shared by many blocks: parts with and without larger sums are
+    joined, by the block that arrives last and by the joining kernel."""
+    say("kv long large values", rows, far, hq, hkv, d, dtype)
+    lens, page = [20000, 3, 7001], 64
+    g = gen(97)
+    need = [-(-n // page) for n in lens]
+    cache = P.kv_cache(sum(need), hkv, d, page=page)
+    table = torch.full((3, max(need)), -1, dtype=torch.int32)
+    ks, vs = [], []
+    for b, n in enumerate(lens):
+        first = sum(need[:b])
+        table[b, :need[b]] = torch.arange(need[b]) + first
+        slots = torch.arange(n, dtype=torch.int32, device="cuda") + first * page
+        k, v = (torch.randn((n, hkv, d), generator=g) for _ in range(2))
+        # (one region of a sequence has them, or all of it)
+        size = 2.0 ** torch.tensor(far)[(torch.arange(n) % 4096 > 2000).long() % len(far)]
+        P.kv_write(cache, k.cuda(), (v * size[:, None, None]).cuda(), slots)
+        k, v = P.kv_read(cache, slots, dtype=F32)
+        ks.append(k.double())
+        vs.append(v.double())
+    counts = rows or [1, 1, 1]
+    starts = [sum(counts[:i]) for i in range(4)]
+    q = (torch.randn((sum(counts), hq, d), generator=g) * 2).to(dtype).cuda()
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    got = P.kv_attention(q, cache, table.cuda(), i32(lens), q_start=None if rows is None else i32(starts))
+    want, bound = kv_paths.attention(q, ks, vs, lens, starts, 0, d ** -0.5)
+    near(got, want.cpu(), bound.cpu() + max(lens) * 2.0 ** -84)
