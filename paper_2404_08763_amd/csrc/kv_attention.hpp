@@ -22,7 +22,7 @@ constexpr float kFar = 8388608.f;
 // 15 + 30 - 48) then), which loses what is below 2^-84 of each token's: fp32's least normal number by a
 // largest weight of 2^(7 - 48).  Else O of kTall or more is made 2^-kLower as large, so that the
 // sum of a row's parts (four waves of 768 blocks at most) stays in range.
-constexpr uint32_t kHighScale = 192;  // 2^65: a byte's upper two bits
+constexpr uint32_t kHighScale = 192;  // 2^65
 constexpr int kLift = 48, kLower = 16;
 constexpr uint32_t kTall = (127u + 112u) << 23;  // 2^112
 
@@ -670,7 +670,7 @@ __device__ __forceinline__ void wide_values(KvSums<D, QT>& w, const KvAttentionA
                                             uint32_t lost = 0) {
   const int lane = threadIdx.x % 64, g = lane / 16;
   uint32_t odd = 0, vs[2] = {scales[0], scales[1]};
-  if (__ballot((((vs[0] & vs[0] << 1) | (vs[1] & vs[1] << 1)) & 0x80808080u) != 0)) w.large = true;
+  bool large = false;  // (those of NaN are none: such rows are NaN however they are done)
   float sc[2][4];
 #pragma unroll
   for (int u = 0; u < 2; ++u)
@@ -679,8 +679,10 @@ __device__ __forceinline__ void wide_values(KvSums<D, QT>& w, const KvAttentionA
       const uint32_t byte = vs[u] >> (8 * i) & 0xffu;
       const bool nan = byte > kKvMaxExp + 127;
       odd |= nan ? 1u << (4 * u + i) : 0u;
+      large |= byte >= kHighScale && !nan;
       sc[u][i] = kv_scale(nan ? 127u : byte);
     }
+  if (__ballot(large)) w.large = true;
   uint32_t nan = 0;  // bit 4 t + i: the row sees a NaN in the columns o[t][..][i]
   if (__ballot(odd != 0)) {
     // Token 16 u + 4 g' + i is NaN in the columns of lane (n', g').  The columns o[..][..][n] of a
