@@ -338,7 +338,7 @@ struct KvAttentionArgs {
   // where there are fewer than blocks (by_tile), else of the block that it begins in
   int4* desc;            // [sums]
   int sums, by_tile;
-  float* part;           // [blocks x 2] partial sums
+  float* part;           // [blocks x 2] partial sums; the first and the last are no memory of the workspace's
 };
 // Workspace of a call, and at most of any call of up to N rows and B sequences.
 size_t kv_attention_bytes(int N, int B, int hq, int hkv, int d, bool bf16, bool planned);

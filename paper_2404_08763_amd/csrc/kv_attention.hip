@@ -148,15 +148,18 @@ struct Shape {
 };
 constexpr size_t up256(size_t v) { return (v + 255) / 256 * 256; }
 constexpr int kMostBlocks = 768;
-size_t part_bytes(int d, int R, int blocks) { return (size_t)blocks * 2 * R * (d + 2) * 4; }
+// Partial sums: two a block, but for the first block's first and the last block's second, which no tile has.
+size_t part_bytes(int d, int R, int blocks) { return (size_t)(2 * blocks - 2) * R * (d + 2) * 4; }
 
-// Two to a compute unit; fewer where a workspace without its lists would pass 64 MiB: 496 for bf16 rows of
-// 128 columns, 504 for 256 columns.  (A bf16 prompt of 4096 rows takes 172 us with 512, 178 with 496, 183 with
-// 480; one of fp32 rows 292 with 512, 308 with 480.)
+// Two to a compute unit; fewer where a workspace without its lists would pass 64 MiB: 504 for bf16 rows of
+// 128 columns and for 256 columns.  (23 bf16 prompts of 512 to 8192 rows of 128 columns take 0.957 of the time
+// of 480 blocks with 512, 0.976 with 504, single ones up to 5% more or 5% less by how tiles fall on blocks;
+// fp32 rows 0.959 with 512; 256 columns 0.996 with 512, 1.01 with 504.)
 constexpr size_t kMostWorkspace = (size_t)64 << 20;
 int prompt_blocks(int d, bool bf16) {
-  const size_t fit = (kMostWorkspace - 256 - up256(kMostBlocks * 40)) / part_bytes(d, kv_prompt_rows(d, bf16), 1);
-  return (int)std::min<size_t>(512, fit / 8 * 8);
+  int blocks = 512;
+  while (256 + up256(kMostBlocks * 40) + part_bytes(d, kv_prompt_rows(d, bf16), blocks) > kMostWorkspace) blocks -= 8;
+  return blocks;
 }
 
 Shape shape_of(int N, int B, int hq, int hkv, int d, bool bf16, bool planned) {
@@ -234,7 +237,7 @@ hipError_t launch_kv_attention(KvAttentionArgs a, int d, bool bf16, hipStream_t 
   a.prefix = reinterpret_cast<int*>(ws + sh.off_prefix);
   a.first = reinterpret_cast<int*>(ws + sh.off_first);
   a.desc = reinterpret_cast<int4*>(ws + sh.off_desc);
-  a.part = reinterpret_cast<float*>(ws + sh.off_part);
+  a.part = reinterpret_cast<float*>(ws + sh.off_part - (size_t)sh.R * (d + 2) * 4);
   a.tiles = a.q_start ? (int)sh.tiles : (a.hq / a.hkv + sh.R - 1) / sh.R;
   // The last block to arrive joins a tile's parts where they are 64 KB at most if all tiles are
   // as long as the tables (tiles of very different lengths: KvRun); more of them a kernel of their own.

@@ -7,7 +7,7 @@
 // is multiplied (two buffers, one barrier a step).  Bound by issue: matrix cores work 0.33, vector ALUs (softmax,
 // the weights' rounding, the conversion) 0.47 of a busy compute unit's cycles, and the two waves
 // of a SIMD hide only a part of one behind the other.  4096 rows of one sequence, 32 heads of
-// 128 columns on 8 (137 GFLOP): 180 us, 0.76 PFLOP/s; in fp32 292.
+// 128 columns on 8 (137 GFLOP): 180 us, 0.76 PFLOP/s; in fp32 288.
 #pragma once
 
 #include "kv_attention.hpp"
@@ -68,7 +68,7 @@ __device__ __forceinline__ bool join_prompt(const KvAttentionArgs& a, KvSums<D, 
   int me = threadIdx.x;
   asm volatile("" : "+v"(me));  // (nothing of this is computed in front of the loop and kept over it)
   const int lane = me % 64, mine = me / 64 * 16 * QT;
-  const __amdgpu_buffer_rsrc_t parts = make_rsrc(a.part, (uint32_t)a.blocks * 2 * (Z::PART * 4));
+  const __amdgpu_buffer_rsrc_t parts = make_rsrc(a.part, (uint32_t)(a.blocks * 2 - 1) * (Z::PART * 4));
   const auto slot = [&](int i) { return (uint32_t)(2 * (first + i) + (i == 0 ? 1 : 0)) * (Z::PART * 4); };
   // a thread's words of a part: its sums, then m and l
   const auto word = [&](int t, int j) { return (uint32_t)((t * J + j) * kKvThreads + me) * 16; };

@@ -317,7 +317,7 @@ __global__ __launch_bounds__(kThreads, (Sizes<D, QT, BF16>::WAVES)) void k_kv_ro
     }
     // where the part goes, in bytes from the first block's
     const uint32_t part = (uint32_t)(run.lb * 2 + (p.head ? 1 : 0)) * (Z::PART * 4);
-    const __amdgpu_buffer_rsrc_t parts = make_rsrc(a.part, (uint32_t)a.blocks * 2 * (Z::PART * 4));
+    const __amdgpu_buffer_rsrc_t parts = make_rsrc(a.part, (uint32_t)(a.blocks * 2 - 1) * (Z::PART * 4));
 #pragma unroll
     for (int t = 0; t < QT; ++t) {
       __syncthreads();
